@@ -191,8 +191,8 @@ def _grown_scale(amax, old, cache):
     old = old.clamp_min(_MIN_SCALE)
     most = old * _QMAX[cache]
     k = (torch.frexp(amax).exponent - torch.frexp(most).exponent).clamp_min(0)
-    k = k + (most * _two(k.clamp_max(127)) < amax)
-    return old * _two(k.clamp_max(127))
+    k = torch.where(amax > most, k + (most * _two(k.clamp_max(126)) < amax), 0)
+    return old * _two(k.clamp_max(126))
 
 
 def _encode(x, cache):
