@@ -106,6 +106,7 @@ typedef enum selkv_rope {
 #define SELKV_DEVERR_TIMEOUT 0x2u  /* a bounded wait gave up; the launch's output is void  */
 #define SELKV_DEVERR_LENGTH 0x4u   /* lengths[b] outside [0, m_cap]; clamped              */
 #define SELKV_DEVERR_COUNT 0x8u    /* compress kept a count other than m_b (internal)     */
+#define SELKV_DEVERR_VALUE 0x10u   /* an infinity or NaN was put into an 8-bit cache       */
 
 typedef struct selkv_shape {
   int32_t dtype;        /* selkv_dtype of K, V, Q_obs, q, k_new, v_new, K_c, V_c and out  */
@@ -345,6 +346,87 @@ SELKV_API selkv_status selkv_decode_attn_static(const selkv_shape* shape, const 
                                                 int32_t* lengths, const void* k_new,
                                                 const void* v_new, void* out,
                                                 uint32_t* flags_out, selkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Caches held in 8 bits.  The paper compresses a cache in tokens; this keeps the rows that are
+ * left (or all rows of an uncompressed cache) in 8 bits an element, with one fp32 scale for each
+ * `block` rows of a KV head of K and of V: element = code * scale.
+ *
+ * Scale and codes of a block, with A the largest finite magnitude of the rows written and qmax the largest
+ * code (448 for e4m3, 127 for int8):
+ *   - a block whose first row is written by the call gets the smallest scale s of a grid with
+ *     s * qmax >= A, at least 2^-100; the grid is the powers of two for e4m3 and m/8 * 2^e, m = 8..15,
+ *     for int8;
+ *   - a block that holds rows already keeps its scale s0 times 2^k, with the smallest k >= 0 that
+ *     covers A; where k > 0 its old codes become round(code * 2^-k) (exact for e4m3 codes that do
+ *     not become subnormal; another rounding of at most half a step for int8);
+ *   - a code is the value nearest to element / s, ties to even.  Infinities become +-qmax, a NaN an e4m3 NaN
+ *     or the int8 code 0; both set SELKV_DEVERR_VALUE.
+ * An element is off by at most s / 2 (int8), or 2^-4 of itself and at least s * 2^-10 (e4m3), and for
+ * int8 by up to s / 2 in all further re-encodings.
+ * ------------------------------------------------------------------------------------- */
+typedef enum selkv_qtype { SELKV_Q_E4M3 = 0, SELKV_Q_INT8 = 1 } selkv_qtype;
+
+typedef struct selkv_qcache {
+  int32_t type;     /* selkv_qtype                                                               */
+  int32_t block;    /* rows that share a scale: 16, 32, 64 or 128                                */
+  void* K;          /* [B][Hkv][m_cap][d] codes                                                  */
+  void* V;          /* [B][Hkv][m_cap][d] codes                                                  */
+  float* K_scale;   /* [B][Hkv][ceil(m_cap / block)]; positive normal numbers where rows are     */
+  float* V_scale;   /* [B][Hkv][ceil(m_cap / block)]                                             */
+  float* bias;      /* [B][Hkv][m_cap] compensation of each row, or NULL (none)                  */
+  int32_t* lengths; /* [B] rows held by each sequence                                            */
+} selkv_qcache;
+
+/* Rows into the cache, as they are produced: a compressed or uncompressed prompt, a chunk, a token.
+ * For every sequence b, rows t < counts[b] of K_new and V_new go to rows lengths[b] + t; bias (if the
+ * cache has one) takes bias_new's entries, or 0; then lengths[b] += counts[b].  An empty cache starts
+ * from lengths = 0 (codes, scales and bias need no initial value).  Rows behind the new length
+ * and scales of blocks without new rows are left as they were.
+ *
+ * rows      row capacity of K_new, V_new and bias_new per (b, kv), at least 1.
+ * K_new, V_new  [B][Hkv][rows][d] of the shape's dtype; bias_new [B][Hkv][rows] fp32 or NULL.
+ * counts    [B] int32 device, 0 .. rows, or NULL: all `rows` rows.  (The lengths that
+ *           selkv_compress wrote are the counts of its K_c, V_c and bias.)  Must not be the
+ *           cache's own lengths.
+ * A sequence whose rows would pass m_cap takes none of them and sets SELKV_DEVERR_CAPACITY; a length
+ * or count out of range is clamped and sets SELKV_DEVERR_LENGTH.
+ * Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor (bias, bias_new and counts may be
+ * NULL), bias_new without a bias, a bad shape, type or block; SELKV_ERR_UNSUPPORTED for d not
+ * in {64, 128}; SELKV_ERR_WORKSPACE when workspace_bytes < selkv_qcache_workspace_size. */
+SELKV_API size_t selkv_qcache_workspace_size(const selkv_shape* shape);
+
+SELKV_API selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv_qcache* cache, int32_t rows,
+                                           const void* K_new, const void* V_new, const float* bias_new,
+                                           const int32_t* counts, void* workspace, size_t workspace_bytes,
+                                           selkv_stream_t stream);
+
+/* Rows back out of the cache: rows row0 .. row0 + rows - 1 of each (b, kv) that lie below lengths[b], as
+ * code * scale rounded once to the shape's dtype, into K_out and V_out [B][Hkv][rows][d].  Rows at
+ * or behind lengths[b] of the outputs are left as they were.  0 <= row0, 1 <= rows,
+ * row0 + rows <= m_cap.  Errors as above. */
+SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cache, int32_t row0,
+                                         int32_t rows, void* K_out, void* V_out, void* workspace,
+                                         size_t workspace_bytes, selkv_stream_t stream);
+
+/* Compensated decode attention over an 8-bit cache: selkv_decode_attn's formula over the values that
+ * the codes stand for,
+ *   out[b][h] = sum_{i < L} softmax_i(q[b][h] . k_i / sqrt(d) + bias_i) * v_i,
+ * plus, when k_new and v_new are given, the new row as given (not rounded to 8 bits) with bias 0.
+ * The new row is then put into the cache as selkv_qcache_append does with one row (bias 0, length
+ * + 1), all inside the call.
+ *
+ * q, out        [B][Hq][d] of the shape's dtype; k_new, v_new [B][Hkv][d] or both NULL.
+ * A row whose bias is -inf has no weight, and a head whose rows all have none gives out = 0, as
+ * does an empty cache without a new row; rows whose bias is the lowest finite number are the limit of very
+ * small weights (rows that all have it share the weight).  An append that would pass m_cap is
+ * skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
+ * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */
+SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);
+
+SELKV_API selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* cache, const void* q,
+                                           const void* k_new, const void* v_new, void* out, void* workspace,
+                                           size_t workspace_bytes, selkv_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -22,5 +22,7 @@ from ._binding import (  # noqa: F401
     selkv_decode_workspace_size, selkv_decode_attn, selkv_decode_attn_static,
     selkv_layer_average_workspace_size, selkv_layer_average_bias, selkv_score_workspace_size,
     selkv_score,
+    SELKV_Q_E4M3, SELKV_Q_INT8, SELKV_DEVERR_VALUE, selkv_qcache, selkv_qcache_workspace_size, selkv_qcache_append,
+    selkv_qcache_read, selkv_decode_q_workspace_size, selkv_decode_attn_q,
     SELKV_STATIC_SCRATCH_BYTES,
 )

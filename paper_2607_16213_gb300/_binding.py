@@ -20,6 +20,8 @@ SELKV_BIAS_RATIO, SELKV_BIAS_COUNT = 0, 1
 SELKV_ROUTE_BUCKET, SELKV_ROUTE_COSINE = 0, 1
 SELKV_SCORE_ROWSTATS, SELKV_SCORE_COLSUMS, SELKV_SCORE_ALL = 1, 2, 3
 SELKV_DEVERR_CAPACITY, SELKV_DEVERR_TIMEOUT, SELKV_DEVERR_LENGTH, SELKV_DEVERR_COUNT = 1, 2, 4, 8
+SELKV_DEVERR_VALUE = 16
+SELKV_Q_E4M3, SELKV_Q_INT8 = 0, 1
 SELKV_MAX_BATCH = 1024
 SELKV_STATIC_SCRATCH_BYTES = 4 << 20
 
@@ -65,6 +67,11 @@ class selkv_compress_debug(ctypes.Structure):
                 ("target", c_vp), ("gate", c_vp), ("decision", c_vp), ("ratio", c_vp)]
 
 
+class selkv_qcache(ctypes.Structure):
+    _fields_ = [("type", c_i32), ("block", c_i32), ("K", c_vp), ("V", c_vp), ("K_scale", c_vp),
+                ("V_scale", c_vp), ("bias", c_vp), ("lengths", c_vp)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 
 
@@ -104,6 +111,14 @@ def library() -> ctypes.CDLL:
                                       c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
         "selkv_decode_attn_static": (c_i32, [ctypes.POINTER(selkv_shape), c_vp, c_vp, c_vp, c_vp,
                                              c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]),
+        "selkv_qcache_workspace_size": (c_sz, [ctypes.POINTER(selkv_shape)]),
+        "selkv_qcache_append": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_qcache), c_i32, c_vp,
+                                        c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
+        "selkv_qcache_read": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_qcache), c_i32, c_i32,
+                                      c_vp, c_vp, c_vp, c_sz, c_vp]),
+        "selkv_decode_q_workspace_size": (c_sz, [ctypes.POINTER(selkv_shape)]),
+        "selkv_decode_attn_q": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_qcache), c_vp, c_vp,
+                                        c_vp, c_vp, c_vp, c_sz, c_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -236,3 +251,35 @@ def selkv_decode_attn_static(shape: selkv_shape, q, K_c, V_c, bias, lengths, k_n
     return library().selkv_decode_attn_static(ctypes.byref(shape), _ptr(q), _ptr(K_c), _ptr(V_c),
                                               _ptr(bias), _ptr(lengths), _ptr(k_new), _ptr(v_new),
                                               _ptr(out), _ptr(flags_out), _stream(stream))
+
+
+def selkv_qcache_workspace_size(shape: selkv_shape) -> int:
+    return int(library().selkv_qcache_workspace_size(ctypes.byref(shape)))
+
+
+def selkv_qcache_append(shape: selkv_shape, cache: selkv_qcache, rows: int, K_new, V_new, bias_new, counts,
+                        workspace, workspace_bytes: int, stream=None) -> int:
+    """See include/selkv.h."""
+    return library().selkv_qcache_append(ctypes.byref(shape), ctypes.byref(cache), int(rows), _ptr(K_new),
+                                         _ptr(V_new), _ptr(bias_new), _ptr(counts), _ptr(workspace),
+                                         int(workspace_bytes), _stream(stream))
+
+
+def selkv_qcache_read(shape: selkv_shape, cache: selkv_qcache, row0: int, rows: int, K_out, V_out, workspace,
+                      workspace_bytes: int, stream=None) -> int:
+    """See include/selkv.h."""
+    return library().selkv_qcache_read(ctypes.byref(shape), ctypes.byref(cache), int(row0), int(rows),
+                                       _ptr(K_out), _ptr(V_out), _ptr(workspace), int(workspace_bytes),
+                                       _stream(stream))
+
+
+def selkv_decode_q_workspace_size(shape: selkv_shape) -> int:
+    return int(library().selkv_decode_q_workspace_size(ctypes.byref(shape)))
+
+
+def selkv_decode_attn_q(shape: selkv_shape, cache: selkv_qcache, q, k_new, v_new, out, workspace,
+                        workspace_bytes: int, stream=None) -> int:
+    """See include/selkv.h."""
+    return library().selkv_decode_attn_q(ctypes.byref(shape), ctypes.byref(cache), _ptr(q), _ptr(k_new),
+                                         _ptr(v_new), _ptr(out), _ptr(workspace), int(workspace_bytes),
+                                         _stream(stream))

@@ -2,6 +2,7 @@
 then call selkv_compress / selkv_decode_attn.  No arithmetic of the method happens here."""
 from __future__ import annotations
 
+import contextlib
 import math
 from dataclasses import dataclass, field
 from typing import Optional, Sequence
@@ -113,4 +114,158 @@ def decode(cache: CompressedCache, q: torch.Tensor, k_new: Optional[torch.Tensor
     st = B.selkv_decode_attn(shape, q, cache.K_c, cache.V_c, cache.bias if use_bias else None,
                              cache.lengths, k_new, v_new, out, ws.buf, ws.nbytes, stream)
     B.check(st, "selkv_decode_attn")
+    return out
+
+
+# ---- caches held in 8 bits ----------------------------------------------------------------------
+_QTYPE = {"e4m3": B.SELKV_Q_E4M3, "int8": B.SELKV_Q_INT8}
+_CODE_DTYPE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+def _bad(what: str) -> None:
+    raise B.SelKVError(B.SELKV_ERR_INVALID_ARG, what)
+
+
+def _tensor(t, name: str, shape, dtype, device) -> None:
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        _bad("%s: a contiguous %s tensor %s on %s is wanted, not %s %s on %s"
+             % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+
+
+@dataclass
+class QuantCache:
+    """A cache held in 8 bits (see selkv_qcache in include/selkv.h): codes [B][Hkv][m_cap][d] in
+    float8_e4m3fn ("e4m3") or int8 ("int8"), a scale for each `block` rows, compensation per row or
+    None, and the rows held.  Contiguous tensors of one device."""
+    shape: B.selkv_shape
+    cache_type: str
+    block: int
+    K: torch.Tensor
+    V: torch.Tensor
+    K_scale: torch.Tensor
+    V_scale: torch.Tensor
+    bias: Optional[torch.Tensor]
+    lengths: torch.Tensor
+
+    def __post_init__(self):
+        s = self.shape
+        if self.cache_type not in _QTYPE or self.block not in (16, 32, 64, 128):
+            _bad("QuantCache: cache_type is e4m3 or int8, block 16, 32, 64 or 128")
+        dev, code = self.K.device, _CODE_DTYPE[self.cache_type]
+        if dev.type != "cuda":
+            _bad("QuantCache: tensors of a CUDA device")
+        rows = (s.batch, s.num_kv_heads, s.m_cap)
+        scales = (s.batch, s.num_kv_heads, -(-s.m_cap // self.block))
+        for name, t, want, dt in (("K", self.K, rows + (s.head_dim,), code), ("V", self.V, rows + (s.head_dim,), code),
+                                  ("K_scale", self.K_scale, scales, torch.float32),
+                                  ("V_scale", self.V_scale, scales, torch.float32),
+                                  ("bias", self.bias, rows, torch.float32), ("lengths", self.lengths, (s.batch,), torch.int32)):
+            if t is not None or name != "bias":
+                _tensor(t, "QuantCache." + name, want, dt, dev)
+        self._dtype = _TORCH_DTYPE[s.dtype]
+        self._bias = self._struct(self.bias)
+        self._plain = self._struct(None) if self.bias is not None else self._bias
+
+    def _struct(self, bias) -> B.selkv_qcache:
+        return B.selkv_qcache(_QTYPE[self.cache_type], self.block, self.K.data_ptr(), self.V.data_ptr(),
+                              self.K_scale.data_ptr(), self.V_scale.data_ptr(),
+                              bias.data_ptr() if bias is not None else None, self.lengths.data_ptr())
+
+
+def alloc_quant(shape: B.selkv_shape, cache_type: str = "e4m3", block: int = 64, bias: bool = True,
+                device="cuda") -> QuantCache:
+    """An empty 8-bit cache."""
+    if cache_type not in _QTYPE or block not in (16, 32, 64, 128):
+        _bad("alloc_quant: cache_type is e4m3 or int8, block 16, 32, 64 or 128")
+    rows = (shape.batch, shape.num_kv_heads, shape.m_cap)
+    scales = (shape.batch, shape.num_kv_heads, -(-shape.m_cap // block))
+    codes = [torch.zeros(rows + (shape.head_dim,), dtype=torch.int8, device=device).view(_CODE_DTYPE[cache_type])
+             for _ in range(2)]
+    return QuantCache(shape, cache_type, block, *codes,
+                      *(torch.zeros(scales, dtype=torch.float32, device=device) for _ in range(2)),
+                      torch.zeros(rows, dtype=torch.float32, device=device) if bias else None,
+                      torch.zeros((shape.batch,), dtype=torch.int32, device=device))
+
+
+@contextlib.contextmanager
+def _on(device: torch.device, stream):
+    """The cache's device current, and its allocations made on the stream that the call runs on."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream().cuda_stream
+            return
+        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        with torch.cuda.stream(s):
+            yield s.cuda_stream
+
+
+def quant_append(cache: QuantCache, K_new: torch.Tensor, V_new: torch.Tensor, bias_new: Optional[torch.Tensor] = None,
+                 counts: Optional[torch.Tensor] = None, workspace: Optional[Workspace] = None, stream=None) -> QuantCache:
+    """selkv_qcache_append: rows [B][Hkv][T][d] (the first counts[b] of each sequence) behind those of
+    the cache, in place."""
+    s, dev = cache.shape, cache.K.device
+    T = K_new.shape[2] if K_new.dim() == 4 else 0
+    want = (s.batch, s.num_kv_heads, T, s.head_dim)
+    _tensor(K_new, "quant_append: K_new", want, cache._dtype, dev)
+    _tensor(V_new, "quant_append: V_new", want, cache._dtype, dev)
+    if bias_new is not None:
+        _tensor(bias_new, "quant_append: bias_new", want[:3], torch.float32, dev)
+    if counts is not None:
+        _tensor(counts, "quant_append: counts", (s.batch,), torch.int32, dev)
+    with _on(dev, stream) as st:
+        ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+        B.check(B.selkv_qcache_append(s, cache._bias, T, K_new, V_new, bias_new, counts, ws.buf, ws.nbytes, st),
+                "selkv_qcache_append")
+    return cache
+
+
+def quantize(cache: CompressedCache, cache_type: str = "e4m3", block: int = 64, workspace: Optional[Workspace] = None,
+             stream=None) -> QuantCache:
+    """The compressed cache in 8 bits: its rows, compensation and lengths in a QuantCache of its capacity."""
+    with _on(cache.K_c.device, stream) as st:
+        q = alloc_quant(cache.shape, cache_type, block, True, cache.K_c.device)
+        return quant_append(q, cache.K_c, cache.V_c, cache.bias, cache.lengths[:cache.shape.batch], workspace, st)
+
+
+def quant_read(cache: QuantCache, row0: int = 0, rows: Optional[int] = None, out=None,
+               workspace: Optional[Workspace] = None, stream=None):
+    """selkv_qcache_read: (K, V) of rows row0 .. row0 + rows - 1, [B][Hkv][rows][d] (with `out` given its
+    rows behind the lengths stay, else they are zeros)."""
+    s, dev = cache.shape, cache.K.device
+    if rows is None:
+        rows = out[0].shape[2] if out is not None else s.m_cap - row0
+    want = (s.batch, s.num_kv_heads, rows, s.head_dim)
+    with _on(dev, stream) as st:
+        if out is None:
+            if rows < 1:
+                _bad("quant_read: rows")
+            out = tuple(torch.zeros(want, dtype=cache._dtype, device=dev) for _ in range(2))
+        K, V = out
+        _tensor(K, "quant_read: K", want, cache._dtype, dev)
+        _tensor(V, "quant_read: V", want, cache._dtype, dev)
+        ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+        B.check(B.selkv_qcache_read(s, cache._bias, row0, rows, K, V, ws.buf, ws.nbytes, st), "selkv_qcache_read")
+    return K, V
+
+
+def decode_quant(cache: QuantCache, q: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+                 v_new: Optional[torch.Tensor] = None, use_bias: bool = True, out: Optional[torch.Tensor] = None,
+                 workspace: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """selkv_decode_attn_q: one token [B][Hq][d] over an 8-bit cache (optionally appending k_new / v_new
+    [B][Hkv][d])."""
+    s, dev = cache.shape, cache.K.device
+    want = (s.batch, s.num_q_heads, s.head_dim)
+    _tensor(q, "decode_quant: q", want, cache._dtype, dev)
+    if k_new is not None and v_new is not None:
+        new = (s.batch, s.num_kv_heads, s.head_dim)
+        _tensor(k_new, "decode_quant: k_new", new, cache._dtype, dev)
+        _tensor(v_new, "decode_quant: v_new", new, cache._dtype, dev)
+    with _on(dev, stream) as st:
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _tensor(out, "decode_quant: out", want, cache._dtype, dev)
+        ws = workspace or Workspace(B.selkv_decode_q_workspace_size(s), dev, st)
+        B.check(B.selkv_decode_attn_q(s, cache._bias if use_bias else cache._plain, q, k_new, v_new, out, ws.buf,
+                                      ws.nbytes, st), "selkv_decode_attn_q")
     return out

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "quant.cuh"
 #include "selkv_internal.cuh"
 
 namespace selkv {
@@ -138,6 +139,53 @@ DecodePlan plan_decode(const selkv_shape& s) {
                    decode_record_floats(s.num_q_heads / s.num_kv_heads, p.splits, s.head_dim) * 4);
   p.total = off;
   return p;
+}
+
+// 8-bit caches: decode.  One arrival counter for each unit of a KV head's query heads
+// (decode_q_units), one for each KV head and one for each sequence.
+struct DecodeQPlan {
+  size_t cnt_head, cnt_kv, cnt_seq, partial, total;
+  int splits;
+};
+
+DecodeQPlan plan_decode_q(const selkv_shape& s) {
+  DecodeQPlan p{};
+  size_t off = sizeof(WsHeader);
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round256(bytes);
+    return o;
+  };
+  const size_t bk = (size_t)s.batch * s.num_kv_heads;
+  p.splits = decode_q_splits(s);
+  p.cnt_head = take(bk * 4);
+  p.cnt_kv = take(bk * 4);
+  p.cnt_seq = take((size_t)s.batch * 4);
+  p.partial = take(bk * decode_record_floats(s.num_q_heads / s.num_kv_heads, p.splits, s.head_dim) * 4);
+  p.total = off;
+  return p;
+}
+
+// SELKV_OK when `c` is a cache of shape `s`, and its kernel form in *q.
+selkv_status qcache_of(const selkv_shape& s, const selkv_qcache* c, QCache* q) {
+  if (c == nullptr || (c->type != SELKV_Q_E4M3 && c->type != SELKV_Q_INT8)) return SELKV_ERR_INVALID_ARG;
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return SELKV_ERR_INVALID_ARG;
+  if (s.m_cap < 1) return SELKV_ERR_INVALID_ARG;
+  const void* tensors[] = {c->K, c->V, c->K_scale, c->V_scale, c->lengths};
+  for (const void* t : tensors)
+    if (t == nullptr || !aligned(t, 16)) return SELKV_ERR_INVALID_ARG;
+  if (c->bias != nullptr && !aligned(c->bias, 16)) return SELKV_ERR_INVALID_ARG;
+  if (s.head_dim != 64 && s.head_dim != 128) return SELKV_ERR_UNSUPPORTED;
+  q->type = c->type;
+  q->block_log2 = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
+  q->nblk = (int)(((int64_t)s.m_cap + c->block - 1) / c->block);
+  q->K = static_cast<uint8_t*>(c->K);
+  q->V = static_cast<uint8_t*>(c->V);
+  q->ks = c->K_scale;
+  q->vs = c->V_scale;
+  q->bias = c->bias;
+  q->lengths = c->lengths;
+  return SELKV_OK;
 }
 
 template <typename T>
@@ -514,6 +562,110 @@ selkv_status selkv_decode_attn(const selkv_shape* shape, const void* q, void* K_
   a.cnt_seq = at<uint32_t>(workspace, plan.cnt_seq);
   a.partial = at<float>(workspace, plan.partial);
   const cudaError_t e = launch_decode(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += kDecodeKernels;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+size_t selkv_qcache_workspace_size(const selkv_shape* shape) {
+  if (!shape_ok(shape)) return 0;
+  return sizeof(WsHeader) + round256((size_t)shape->batch * 4);
+}
+
+selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv_qcache* cache, int32_t rows, const void* K_new,
+                                 const void* V_new, const float* bias_new, const int32_t* counts, void* workspace,
+                                 size_t workspace_bytes, selkv_stream_t stream) {
+  if (!shape_ok(shape)) return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  QAppendArgs a{};
+  if (const selkv_status st = qcache_of(s, cache, &a.c); st != SELKV_OK) return st;
+  if (rows < 1 || K_new == nullptr || V_new == nullptr || !aligned(K_new, 16) || !aligned(V_new, 16))
+    return SELKV_ERR_INVALID_ARG;
+  if (bias_new != nullptr && (cache->bias == nullptr || !aligned(bias_new, 16))) return SELKV_ERR_INVALID_ARG;
+  if (counts != nullptr && (!aligned(counts, 4) || counts == cache->lengths)) return SELKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SELKV_ERR_WORKSPACE;
+  if (workspace_bytes < selkv_qcache_workspace_size(shape)) return SELKV_ERR_WORKSPACE;
+  a.dtype = s.dtype;
+  a.B = s.batch;
+  a.Hkv = s.num_kv_heads;
+  a.D = s.head_dim;
+  a.m_cap = s.m_cap;
+  a.rows = rows;
+  a.k_new = K_new;
+  a.v_new = V_new;
+  a.bias_new = bias_new;
+  a.counts = counts;
+  a.flags = at<uint32_t>(workspace, 0);
+  a.cnt_seq = at<uint32_t>(workspace, sizeof(WsHeader));
+  const cudaError_t e = launch_qappend(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 1;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cache, int32_t row0, int32_t rows,
+                               void* K_out, void* V_out, void* workspace, size_t workspace_bytes,
+                               selkv_stream_t stream) {
+  if (!shape_ok(shape)) return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  QReadArgs a{};
+  if (const selkv_status st = qcache_of(s, cache, &a.c); st != SELKV_OK) return st;
+  if (row0 < 0 || rows < 1 || (int64_t)row0 + rows > s.m_cap) return SELKV_ERR_INVALID_ARG;
+  if (K_out == nullptr || V_out == nullptr || !aligned(K_out, 16) || !aligned(V_out, 16)) return SELKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return SELKV_ERR_WORKSPACE;
+  if (workspace_bytes < selkv_qcache_workspace_size(shape)) return SELKV_ERR_WORKSPACE;
+  a.dtype = s.dtype;
+  a.B = s.batch;
+  a.Hkv = s.num_kv_heads;
+  a.D = s.head_dim;
+  a.m_cap = s.m_cap;
+  a.row0 = row0;
+  a.rows = rows;
+  a.k_out = K_out;
+  a.v_out = V_out;
+  a.flags = at<uint32_t>(workspace, 0);
+  const cudaError_t e = launch_qread(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 1;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+size_t selkv_decode_q_workspace_size(const selkv_shape* shape) {
+  if (!shape_ok(shape)) return 0;
+  return plan_decode_q(*shape).total;
+}
+
+selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* cache, const void* q, const void* k_new,
+                                 const void* v_new, void* out, void* workspace, size_t workspace_bytes,
+                                 selkv_stream_t stream) {
+  if (!shape_ok(shape)) return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  QDecodeArgs a{};
+  if (const selkv_status st = qcache_of(s, cache, &a.c); st != SELKV_OK) return st;
+  if (q == nullptr || out == nullptr || !aligned(q, 16) || !aligned(out, 16)) return SELKV_ERR_INVALID_ARG;
+  if ((k_new == nullptr) != (v_new == nullptr)) return SELKV_ERR_INVALID_ARG;
+  if (k_new != nullptr && (!aligned(k_new, 16) || !aligned(v_new, 16))) return SELKV_ERR_INVALID_ARG;
+  if ((int64_t)s.batch * s.num_kv_heads * s.m_cap >= (int64_t)1 << 31) return SELKV_ERR_UNSUPPORTED;
+  const DecodeQPlan plan = plan_decode_q(s);
+  if (workspace == nullptr || !aligned(workspace, 256)) return SELKV_ERR_WORKSPACE;
+  if (workspace_bytes < plan.total) return SELKV_ERR_WORKSPACE;
+  a.dtype = s.dtype;
+  a.B = s.batch;
+  a.Hq = s.num_q_heads;
+  a.Hkv = s.num_kv_heads;
+  a.G = s.num_q_heads / s.num_kv_heads;
+  a.D = s.head_dim;
+  a.m_cap = s.m_cap;
+  a.splits = plan.splits;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s.head_dim));
+  a.q = q;
+  a.bias = cache->bias;
+  a.lengths = cache->lengths;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.out = out;
+  a.flags = at<uint32_t>(workspace, 0);
+  a.cnt_head = at<uint32_t>(workspace, plan.cnt_head);
+  a.cnt_seq = at<uint32_t>(workspace, plan.cnt_seq);
+  a.partial = at<float>(workspace, plan.partial);
+  const cudaError_t e = launch_decode_q(a, reinterpret_cast<cudaStream_t>(stream));
   g_launches += kDecodeKernels;
   return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
 }

@@ -1,0 +1,202 @@
+// Writing rows into an 8-bit cache and reading them back (quant.cuh has the scales and codes).
+//
+// Append: a CTA takes 128 rows of the cache, aligned to 128, of one KV head's K or V: whole blocks, so
+// no two CTAs share a scale.  A warp takes 16 of the rows and keeps them in registers between the
+// largest magnitude and the codes: an element is read once and a code written once.  Read: a thread takes 16
+// codes at a time.  Both are bound by HBM.
+#include "quant.cuh"
+
+namespace selkv {
+namespace {
+
+constexpr int kTileRows = 128, kWarpRows = 16, kAppendThreads = 256;
+
+template <int TYPE, typename T, int D>
+__global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) {
+  using C = Code<TYPE>;
+  constexpr int kEl = 16 / sizeof(T);           // elements of a 16-byte load
+  constexpr int kLpr = D / kEl;                 // lanes per row
+  constexpr int kRpl = 32 / kLpr;               // rows per load
+  constexpr int kLoads = kWarpRows / kRpl;
+  __shared__ float wmax[kTileRows / kWarpRows];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
+  const size_t bk = (size_t)b * a.Hkv + h;
+  int L = a.c.lengths[b], n = a.counts != nullptr ? a.counts[b] : a.rows;
+  const bool first_cta = blockIdx.x == 0 && h == 0 && isv == 0;
+  if (L < 0 || L > a.m_cap || n < 0 || n > a.rows) {
+    if (tid == 0 && first_cta) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
+    L = min(max(L, 0), a.m_cap);
+    n = min(max(n, 0), a.rows);
+  }
+  if (n > a.m_cap - L) {
+    if (tid == 0 && first_cta) raise_flag(a.flags, SELKV_DEVERR_CAPACITY);
+    n = 0;
+  }
+  const int row0 = (L / kTileRows + (int)blockIdx.x) * kTileRows + warp * kWarpRows;  // this warp's first row
+  const T* src = static_cast<const T*>(isv ? a.v_new : a.k_new) + bk * a.rows * D;
+  uint8_t* codes = (isv ? a.c.V : a.c.K) + bk * a.m_cap * D;
+  float* scales = (isv ? a.c.vs : a.c.ks) + bk * a.c.nblk;
+  float x[kLoads][kEl];
+  float m = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int row = row0 + i * kRpl + lane / kLpr;
+    if (row >= L && row < L + n) {
+      const T* p = src + (size_t)(row - L) * D + (lane % kLpr) * kEl;
+      if constexpr (kEl == 8) load8(p, x[i]);
+      else load4(p, x[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEl; ++e) x[i][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int e = 0; e < kEl; ++e) m = fmaxf(m, finite_abs(x[i][e], &odd));
+  if (odd) raise_flag(a.flags, SELKV_DEVERR_VALUE);
+  m = warp_max(m);
+  if (lane == 0) wmax[warp] = m;
+  const int blk = row0 >> a.c.block_log2, bfirst = blk << a.c.block_log2;
+  const int bend = bfirst + (1 << a.c.block_log2);
+  const bool live = bfirst < L + n && bend > L;  // the block takes new rows (n > 0)
+  const bool holds = live && L > bfirst;
+  const float s0 = holds ? fmaxf(scales[blk], kMinScale) : 0.f;  // read by every warp before one writes it
+  __syncthreads();
+  if (live && n > 0) {
+    const int wpb = (1 << a.c.block_log2) / kWarpRows;  // warps of a block
+    const int w0 = warp / wpb * wpb;
+    m = 0.f;
+    for (int w = w0; w < w0 + wpb; ++w) m = fmaxf(m, wmax[w]);
+    const float s = holds ? grown_scale<TYPE>(s0, m) : C::fresh_scale(m);
+    if (warp == w0 && lane == 0) scales[blk] = s;
+    if (holds && s != s0) {  // this warp's rows among those the block holds, under the new scale
+      const float f = s0 / s;
+      uint32_t* w = reinterpret_cast<uint32_t*>(codes + (size_t)row0 * D);
+      const int old = min(L - row0, kWarpRows);
+      for (int i = lane; i < old * (D / 4); i += 32) {
+        float y[4];
+        C::unpack4(w[i], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] *= f;
+        w[i] = C::pack4(y);
+      }
+    }
+    const float rcp = 1.f / s;
+    const bool any_scale = holds || sizeof(T) == 4;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int row = row0 + i * kRpl + lane / kLpr;
+      if (row < L || row >= L + n) continue;
+      uint32_t w[kEl / 4];
+#pragma unroll
+      for (int j = 0; j < kEl / 4; ++j) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = C::quotient(x[i][j * 4 + e], s, rcp, any_scale);
+        w[j] = C::pack4(y);
+      }
+      uint8_t* dst = codes + (size_t)row * D + (lane % kLpr) * kEl;
+      if constexpr (kEl == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+      else *reinterpret_cast<uint32_t*>(dst) = w[0];
+    }
+  }
+  if (!isv && a.c.bias != nullptr) {
+    const int row = row0 + lane;
+    if (lane < kWarpRows && row >= L && row < L + n)
+      a.c.bias[bk * a.m_cap + row] = a.bias_new != nullptr ? a.bias_new[bk * a.rows + row - L] : 0.f;
+  }
+  // every CTA of the sequence has read its length by the time the last one moves it
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t all = gridDim.x * gridDim.y * 2u;
+    if (atom_add_acq_rel_gpu(&a.cnt_seq[b], 1u) == all - 1u) {
+      a.cnt_seq[b] = 0u;
+      if (n > 0) a.c.lengths[b] = L + n;
+    }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]);
+template <>
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(p) =
+      make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+template <>
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+constexpr int kReadThreads = 256;
+
+template <int TYPE, typename T, int D>
+__global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
+  using C = Code<TYPE>;
+  const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
+  const size_t bk = (size_t)b * a.Hkv + h;
+  int L = a.c.lengths[b];
+  if (L < 0 || L > a.m_cap) {
+    if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && isv == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
+    L = min(max(L, 0), a.m_cap);
+  }
+  const int n = min(a.rows, L - a.row0);  // rows to read (none: <= 0)
+  const uint8_t* codes = (isv ? a.c.V : a.c.K) + (bk * a.m_cap + a.row0) * D;
+  const float* scales = (isv ? a.c.vs : a.c.ks) + bk * a.c.nblk;
+  T* out = static_cast<T*>(isv ? a.v_out : a.k_out) + bk * a.rows * D;
+  const int i = blockIdx.x * kReadThreads + threadIdx.x;  // 16 codes each
+  const int row = i / (D / 16);
+  if (row >= n) return;
+  const uint4 w = *reinterpret_cast<const uint4*>(codes + (size_t)i * 16);
+  const float s = scales[(a.row0 + row) >> a.c.block_log2];
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float y[8], t[4];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      C::unpack4(ws[j * 2 + p], t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[p * 4 + e] = t[e] * s;
+    }
+    store8(out + (size_t)i * 16 + j * 8, y);
+  }
+}
+
+template <int TYPE, typename T>
+cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
+  // the rows behind any length touch at most this many tiles
+  const dim3 grid((a.rows + kTileRows - 2) / kTileRows + 1, a.Hkv, 2 * a.B);
+  if (a.D == 128) qappend_kernel<TYPE, T, 128><<<grid, kAppendThreads, 0, st>>>(a);
+  else qappend_kernel<TYPE, T, 64><<<grid, kAppendThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <int TYPE, typename T>
+cudaError_t qread_t(const QReadArgs& a, cudaStream_t st) {
+  const int per = kReadThreads * 16 / a.D;  // rows of a CTA
+  const dim3 grid((a.rows + per - 1) / per, a.Hkv, 2 * a.B);
+  if (a.D == 128) qread_kernel<TYPE, T, 128><<<grid, kReadThreads, 0, st>>>(a);
+  else qread_kernel<TYPE, T, 64><<<grid, kReadThreads, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_qappend(const QAppendArgs& a, cudaStream_t st) {
+  if (a.c.type == SELKV_Q_E4M3)
+    return a.dtype == SELKV_BF16 ? qappend_t<SELKV_Q_E4M3, __nv_bfloat16>(a, st) : qappend_t<SELKV_Q_E4M3, float>(a, st);
+  return a.dtype == SELKV_BF16 ? qappend_t<SELKV_Q_INT8, __nv_bfloat16>(a, st) : qappend_t<SELKV_Q_INT8, float>(a, st);
+}
+
+cudaError_t launch_qread(const QReadArgs& a, cudaStream_t st) {
+  if (a.c.type == SELKV_Q_E4M3)
+    return a.dtype == SELKV_BF16 ? qread_t<SELKV_Q_E4M3, __nv_bfloat16>(a, st) : qread_t<SELKV_Q_E4M3, float>(a, st);
+  return a.dtype == SELKV_BF16 ? qread_t<SELKV_Q_INT8, __nv_bfloat16>(a, st) : qread_t<SELKV_Q_INT8, float>(a, st);
+}
+
+}  // namespace selkv
