@@ -156,12 +156,13 @@ DecodeQPlan plan_decode_q(const selkv_shape& s) {
     off += round256(bytes);
     return o;
   };
+  const int G = s.num_q_heads / s.num_kv_heads, units = decode_q_units(s.dtype, G);
   const size_t bk = (size_t)s.batch * s.num_kv_heads;
   p.splits = decode_q_splits(s);
-  p.cnt_head = take(bk * 4);
+  p.cnt_head = take(bk * units * 4);
   p.cnt_kv = take(bk * 4);
   p.cnt_seq = take((size_t)s.batch * 4);
-  p.partial = take(bk * decode_record_floats(s.num_q_heads / s.num_kv_heads, p.splits, s.head_dim) * 4);
+  p.partial = take(bk * units * decode_record_floats(units > 1 ? 8 : G, p.splits, s.head_dim) * 4);
   p.total = off;
   return p;
 }
@@ -663,6 +664,7 @@ selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* c
   a.out = out;
   a.flags = at<uint32_t>(workspace, 0);
   a.cnt_head = at<uint32_t>(workspace, plan.cnt_head);
+  a.cnt_kv = at<uint32_t>(workspace, plan.cnt_kv);
   a.cnt_seq = at<uint32_t>(workspace, plan.cnt_seq);
   a.partial = at<float>(workspace, plan.partial);
   const cudaError_t e = launch_decode_q(a, reinterpret_cast<cudaStream_t>(stream));

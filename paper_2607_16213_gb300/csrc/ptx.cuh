@@ -10,6 +10,8 @@ namespace selkv {
 // Rows of d bf16 elements as a 2D tensor for TMA: boxes of 64 elements (128 bytes) x box_rows
 // rows, 128-byte swizzle, zero fill out of bounds.  Host only.
 bool encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, int box_rows);
+// Rows of d bytes (64 or 128): boxes of whole rows, swizzled over their width.  Host only.
+bool encode_rows_u8(CUtensorMap* map, const void* base, uint64_t rows, int d, int box_rows);
 
 // Bounded waits: try_wait suspends for a hardware-chosen slice per call; this many calls is
 // well over a second, after which the caller reports SELKV_DEVERR_TIMEOUT instead of hanging.

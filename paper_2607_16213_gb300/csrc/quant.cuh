@@ -153,7 +153,10 @@ cudaError_t launch_qread(const QReadArgs& a, cudaStream_t s);
 // Decode over an 8-bit cache: DecodeArgs without Kc and Vc.
 struct QDecodeArgs : DecodeArgs {
   QCache c;
+  uint32_t* cnt_kv;  // [B][Hkv] units of a KV head that are done (self-resetting)
 };
+// Units of a KV head: its query heads that one CTA takes together.
+int decode_q_units(int dtype, int G);
 int decode_q_splits(const selkv_shape& s);
 cudaError_t launch_decode_q(const QDecodeArgs& a, cudaStream_t s);
 

@@ -89,10 +89,10 @@ def append_head(val, scale, x, L, block, kind):
 
 
 def decode_head(q, k, v, bias):
-    """q [G][d], k, v [n][d], bias [n] or None -> (out [G][d], sum p|v|, the largest sum_j |q_j k_j| / sqrt(d) and |logit|)."""
+    """q [G][d], k, v [n][d], bias [n] or None -> (out [G][d], sum p|v|, the largest sum_j |q_j k_j| / sqrt(d) and |logit|, p)."""
     G, d = q.shape
     if k.shape[0] == 0:
-        return np.zeros((G, d)), np.zeros((G, d)), 0.0, 0.0
+        return np.zeros((G, d)), np.zeros((G, d)), 0.0, 0.0, np.zeros((G, 0))
     s = q @ k.T / math.sqrt(d)
     mag = (np.abs(q) @ np.abs(k).T / math.sqrt(d)).max()
     if bias is not None:
@@ -103,4 +103,4 @@ def decode_head(q, k, v, bias):
     z = p.sum(1, keepdims=True)
     p = p / np.where(z > 0, z, 1.0)
     fin = np.abs(s[np.isfinite(s)])
-    return p @ v, p @ np.abs(v), mag, (fin[fin < 1e30].max() if (fin < 1e30).any() else 0.0)
+    return p @ v, p @ np.abs(v), mag, (fin[fin < 1e30].max() if (fin < 1e30).any() else 0.0), p

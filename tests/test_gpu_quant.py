@@ -222,17 +222,23 @@ def test_read(kind, dtype, d, block, cap, lens, row0, n):
 
 
 # ---- decode -----------------------------------------------------------------------------------------
-def bound(dtype, want, pv, mag, x, n):
+def bound(dtype, want, pv, mag, x, n, floor):
     """How far a result may be off, from the roundings on its way, with u = 2^-24.  A logit: products of d
     terms summed in fp32 (at most (d + 8) u of sum |q k|; the sum of a chunk may be cut off instead of rounded, hence
     twice that), a query held as fp16 (bf16 queries: exactly; fp32: two halves, 2^-22), and the scale, bias and
     exponential, 8 u of the logit and 4 u.  Each p is off by as much relatively, and so is the normaliser:
     twice.  Weights rounded to fp16 (bf16 caches: 2^-11; fp32: two halves, 2^-21), a fold of n / 8 + 200
-    sums, and the rounding of the output itself."""
+    sums, and the rounding of the output itself.
+    Weights below the normal fp16 range: the kernel holds p vs (p the weight, vs the row's scale) in units of
+    U 2^-10, where U is at most the largest weight of a tile of 32 rows times the largest scale of its rows.  An
+    fp16 below 2^-14 is a multiple of 2^-24, so such a weight is off by at most 2^-25 units, 2^-35 U, whatever its own size.
+    Times a code of at most qmax, over n rows: `floor` = n qmax 2^-35 U.  (It matters where the rows of all
+    large weights hold a code 0, as int8 rows do: an element of 1e-15 next to others of 1 has no digits of its
+    own.)"""
     u = 2.0 ** -24
     dlogit = 2 * (128 + 8) * u * mag + (2.0 ** -22 * mag if dtype == "fp32" else 0.0) + 8 * u * x + 4 * u
     w = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -21
-    return (2 * dlogit + w + (n / 8 + 200) * u) * pv + np.abs(want) * (2.0 ** -8 if dtype == "bf16" else u) + 1e-37
+    return (2 * dlogit + w + (n / 8 + 200) * u) * pv + np.abs(want) * (2.0 ** -8 if dtype == "bf16" else u) + floor + 1e-37
 
 
 def check_out(c, model, out, q, app=None, k=None, v=None, use_bias=True):
@@ -247,9 +253,13 @@ def check_out(c, model, out, q, app=None, k=None, v=None, use_bias=True):
             if k is not None and app[b]:
                 kk, vv = np.vstack([kk, np64(k)[b, h]]), np.vstack([vv, np64(v)[b, h]])
                 bias = np.append(bias, 0.0) if bias is not None else None
-            want, pv, mag, x = R.decode_head(qs[b, h * G:(h + 1) * G], kk, vv, bias)
+            want, pv, mag, x, p = R.decode_head(qs[b, h * G:(h + 1) * G], kk, vv, bias)
             err = np.abs(got[b, h * G:(h + 1) * G] - want)
-            lim = bound(dtype, want, pv, mag, x, kk.shape[0])
+            n = int(model.L[b])
+            at = np.arange(0, n, 32)
+            top = np.maximum.reduceat(p[:, :n], at, 1) * np.maximum.reduceat(model.vs[b, h][np.arange(n) // model.block], at) if n else np.zeros((G, 1))
+            floor = n * R.QMAX[model.kind] * 2.0 ** -35 * top.max(1)[:, None]
+            lim = bound(dtype, want, pv, mag, x, kk.shape[0], floor)
             assert (err <= lim).all(), (b, h, float((err / lim).max()), float(err.max()))
 
 
