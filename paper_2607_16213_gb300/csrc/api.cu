@@ -141,11 +141,10 @@ DecodePlan plan_decode(const selkv_shape& s) {
   return p;
 }
 
-// 8-bit caches: decode.  One arrival counter for each unit of a KV head's query heads
-// (decode_q_units), one for each KV head and one for each sequence.
+// Decode over 8-bit caches.
 struct DecodeQPlan {
-  size_t cnt_head, cnt_kv, cnt_seq, partial, total;
-  int splits;
+  size_t cnt_head, cnt_seq, partial, total;
+  int splits, warps, cluster;
 };
 
 DecodeQPlan plan_decode_q(const selkv_shape& s) {
@@ -156,13 +155,15 @@ DecodeQPlan plan_decode_q(const selkv_shape& s) {
     off += round256(bytes);
     return o;
   };
-  const int G = s.num_q_heads / s.num_kv_heads, units = decode_q_units(s.dtype, G);
   const size_t bk = (size_t)s.batch * s.num_kv_heads;
-  p.splits = decode_q_splits(s);
-  p.cnt_head = take(bk * units * 4);
-  p.cnt_kv = take(bk * 4);
+  const QDecodePlan q = decode_q_plan(s);
+  p.splits = q.splits;
+  p.warps = q.warps;
+  p.cluster = q.cluster;
+  const int clusters = q.splits / q.cluster;
+  p.cnt_head = take(bk * q.cluster * 4);
   p.cnt_seq = take((size_t)s.batch * 4);
-  p.partial = take(bk * units * decode_record_floats(units > 1 ? 8 : G, p.splits, s.head_dim) * 4);
+  p.partial = take(clusters > 1 ? bk * decode_q_record_floats(s.num_q_heads / s.num_kv_heads, q.cluster, clusters, s.head_dim) * 4 : 0);
   p.total = off;
   return p;
 }
@@ -664,7 +665,8 @@ selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* c
   a.out = out;
   a.flags = at<uint32_t>(workspace, 0);
   a.cnt_head = at<uint32_t>(workspace, plan.cnt_head);
-  a.cnt_kv = at<uint32_t>(workspace, plan.cnt_kv);
+  a.warps = plan.warps;
+  a.cluster = plan.cluster;
   a.cnt_seq = at<uint32_t>(workspace, plan.cnt_seq);
   a.partial = at<float>(workspace, plan.partial);
   const cudaError_t e = launch_decode_q(a, reinterpret_cast<cudaStream_t>(stream));

@@ -11,6 +11,66 @@ namespace {
 
 constexpr int kTileRows = 128, kWarpRows = 16, kAppendThreads = 256;
 
+// Four consecutive elements of 16 loaded bytes.
+__device__ __forceinline__ void elements4(const uint4& w, int half, __nv_bfloat16, float (&x)[4]) {
+  const uint32_t a = half ? w.z : w.x, b = half ? w.w : w.y;
+  x[0] = bf16_lo(a), x[1] = bf16_hi(a), x[2] = bf16_lo(b), x[3] = bf16_hi(b);
+}
+__device__ __forceinline__ void elements4(const uint4& w, int, float, float (&x)[4]) {
+  x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+}
+// Bits of the largest magnitude of 16 loaded bytes as an fp32 number (magnitudes order as their bits do;
+// infinities and NaN above the finite ones).
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+template <typename T, int N>
+__device__ __forceinline__ uint32_t max_bits(const uint4 (&w)[N]) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 2) m = max_u16x2(m, u[k] & 0x7fff7fffu);
+      else m = max(m, u[k] & 0x7fffffffu);
+    }
+  }
+  if constexpr (sizeof(T) == 2) m = max(m << 16, m & 0xffff0000u);
+  return m;
+}
+// The largest finite magnitude (where some elements are not).
+template <typename T, int N>
+__device__ __forceinline__ uint32_t max_finite_bits(const uint4 (&w)[N]) {
+  float m = 0.f;
+  bool odd = false;
+  for (int i = 0; i < N; ++i)
+    for (int k = 0; k < (sizeof(T) == 2 ? 2 : 1); ++k) {
+      float x[4];
+      elements4(w[i], k, T{}, x);
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_abs(x[e], &odd));
+    }
+  return __float_as_uint(m);
+}
+// Four finite bf16 elements as codes under a scale of the grid.
+template <int TYPE>
+__device__ __forceinline__ uint32_t encode4(const float (&x)[4], float s, float rcp) {
+  if constexpr (TYPE == SELKV_Q_E4M3) {
+    return cvt_e4m3x2(x[0] * rcp, x[1] * rcp) | cvt_e4m3x2(x[2] * rcp, x[3] * rcp) << 16;
+  } else {
+    // the integer nearest to the quotient is in the low bits of quotient + 1.5 * 2^23
+    uint32_t t[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float q = x[e] * rcp;
+      t[e] = __float_as_uint(fmaf(fmaf(-q, s, x[e]), rcp, q) + 12582912.f);
+    }
+    return __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
+  }
+}
+
 template <int TYPE, typename T, int D>
 __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) {
   using C = Code<TYPE>;
@@ -18,7 +78,7 @@ __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) 
   constexpr int kLpr = D / kEl;                 // lanes per row
   constexpr int kRpl = 32 / kLpr;               // rows per load
   constexpr int kLoads = kWarpRows / kRpl;
-  __shared__ float wmax[kTileRows / kWarpRows];
+  __shared__ uint32_t wmax[kTileRows / kWarpRows];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
   const size_t bk = (size_t)b * a.Hkv + h;
@@ -33,89 +93,85 @@ __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) 
     if (tid == 0 && first_cta) raise_flag(a.flags, SELKV_DEVERR_CAPACITY);
     n = 0;
   }
-  const int row0 = (L / kTileRows + (int)blockIdx.x) * kTileRows + warp * kWarpRows;  // this warp's first row
+  const int tile0 = (L / kTileRows + (int)blockIdx.x) * kTileRows;
+  const int row0 = tile0 + warp * kWarpRows;  // this warp's first row
   const T* src = static_cast<const T*>(isv ? a.v_new : a.k_new) + bk * a.rows * D;
   uint8_t* codes = (isv ? a.c.V : a.c.K) + bk * a.m_cap * D;
   float* scales = (isv ? a.c.vs : a.c.ks) + bk * a.c.nblk;
-  float x[kLoads][kEl];
-  float m = 0.f;
-  bool odd = false;
+  const int at = lane % kLpr * kEl;  // this lane's elements of its rows
+  uint4 x[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int row = row0 + i * kRpl + lane / kLpr;
-    if (row >= L && row < L + n) {
-      const T* p = src + (size_t)(row - L) * D + (lane % kLpr) * kEl;
-      if constexpr (kEl == 8) load8(p, x[i]);
-      else load4(p, x[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEl; ++e) x[i][e] = 0.f;
-    }
+    x[i] = row >= L && row < L + n ? *reinterpret_cast<const uint4*>(src + (size_t)(row - L) * D + at) : make_uint4(0, 0, 0, 0);
   }
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-    for (int e = 0; e < kEl; ++e) m = fmaxf(m, finite_abs(x[i][e], &odd));
-  if (odd) raise_flag(a.flags, SELKV_DEVERR_VALUE);
-  m = warp_max(m);
-  if (lane == 0) wmax[warp] = m;
-  const int blk = row0 >> a.c.block_log2, bfirst = blk << a.c.block_log2;
-  const int bend = bfirst + (1 << a.c.block_log2);
-  const bool live = bfirst < L + n && bend > L;  // the block takes new rows (n > 0)
-  const bool holds = live && L > bfirst;
-  const float s0 = holds ? fmaxf(scales[blk], kMinScale) : 0.f;  // read by every warp before one writes it
-  __syncthreads();
-  if (live && n > 0) {
-    const int wpb = (1 << a.c.block_log2) / kWarpRows;  // warps of a block
-    const int w0 = warp / wpb * wpb;
-    m = 0.f;
-    for (int w = w0; w < w0 + wpb; ++w) m = fmaxf(m, wmax[w]);
-    const float s = holds ? grown_scale<TYPE>(s0, m) : C::fresh_scale(m);
-    if (warp == w0 && lane == 0) scales[blk] = s;
-    if (holds && s != s0) {  // this warp's rows among those the block holds, under the new scale
-      const float f = s0 / s;
-      uint32_t* w = reinterpret_cast<uint32_t*>(codes + (size_t)row0 * D);
-      const int old = min(L - row0, kWarpRows);
-      for (int i = lane; i < old * (D / 4); i += 32) {
-        float y[4];
-        C::unpack4(w[i], y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] *= f;
-        w[i] = C::pack4(y);
-      }
-    }
-    const float rcp = 1.f / s;
-    const bool any_scale = holds || sizeof(T) == 4;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = row0 + i * kRpl + lane / kLpr;
-      if (row < L || row >= L + n) continue;
-      uint32_t w[kEl / 4];
-#pragma unroll
-      for (int j = 0; j < kEl / 4; ++j) {
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = C::quotient(x[i][j * 4 + e], s, rcp, any_scale);
-        w[j] = C::pack4(y);
-      }
-      uint8_t* dst = codes + (size_t)row * D + (lane % kLpr) * kEl;
-      if constexpr (kEl == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-      else *reinterpret_cast<uint32_t*>(dst) = w[0];
-    }
-  }
-  if (!isv && a.c.bias != nullptr) {
-    const int row = row0 + lane;
-    if (lane < kWarpRows && row >= L && row < L + n)
-      a.c.bias[bk * a.m_cap + row] = a.bias_new != nullptr ? a.bias_new[bk * a.rows + row - L] : 0.f;
-  }
-  // every CTA of the sequence has read its length by the time the last one moves it
-  __syncthreads();
-  if (tid == 0) {
+  // The last CTA of the sequence to have read its length moves it: every one has read it by then.
+  if (tid == kAppendThreads - 1) {
     const uint32_t all = gridDim.x * gridDim.y * 2u;
     if (atom_add_acq_rel_gpu(&a.cnt_seq[b], 1u) == all - 1u) {
       a.cnt_seq[b] = 0u;
       if (n > 0) a.c.lengths[b] = L + n;
     }
+  }
+  if (n == 0 || tile0 >= L + n) return;
+  uint32_t m = __reduce_max_sync(0xffffffffu, max_bits<T>(x));
+  const bool finite = __syncthreads_or(m >= 0x7f800000u) == 0;
+  if (!finite) {
+    if (lane == 0 && m >= 0x7f800000u) raise_flag(a.flags, SELKV_DEVERR_VALUE);
+    m = __reduce_max_sync(0xffffffffu, max_finite_bits<T>(x));
+  }
+  if (lane == 0) wmax[warp] = m;
+  const int blk = row0 >> a.c.block_log2, bfirst = blk << a.c.block_log2;
+  const bool live = bfirst < L + n && bfirst + (1 << a.c.block_log2) > L;  // the block takes new rows
+  const bool holds = live && L > bfirst;
+  const float s0 = holds ? fmaxf(scales[blk], kMinScale) : 0.f;  // read by every warp before one writes it
+  __syncthreads();
+  if (!isv && a.c.bias != nullptr) {
+    const int row = row0 + lane;
+    if (lane < kWarpRows && row >= L && row < L + n)
+      a.c.bias[bk * a.m_cap + row] = a.bias_new != nullptr ? a.bias_new[bk * a.rows + row - L] : 0.f;
+  }
+  if (!live) return;
+  const int wpb = (1 << a.c.block_log2) / kWarpRows, w0 = warp / wpb * wpb;  // warps of the block
+  m = 0u;
+  for (int w = w0; w < w0 + wpb; ++w) m = max(m, wmax[w]);
+  const float amax = __uint_as_float(m);
+  const float s = holds ? grown_scale<TYPE>(s0, amax) : C::fresh_scale(amax);
+  if (warp == w0 && lane == 0) scales[blk] = s;
+  if (holds && s != s0) {  // this warp's rows among those the block holds, under the new scale
+    const float f = s0 / s;
+    uint32_t* w = reinterpret_cast<uint32_t*>(codes + (size_t)row0 * D);
+    const int old = min(L - row0, kWarpRows);
+    for (int i = lane; i < old * (D / 4); i += 32) {
+      float y[4];
+      C::unpack4(w[i], y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= f;
+      w[i] = C::pack4(y);
+    }
+  }
+  const float rcp = 1.f / s;
+  const bool any_scale = holds || sizeof(T) == 4, quick = finite && !any_scale;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int row = row0 + i * kRpl + lane / kLpr;
+    if (row < L || row >= L + n) continue;
+    uint32_t w[kEl / 4];
+#pragma unroll
+    for (int j = 0; j < kEl / 4; ++j) {
+      float y[4];
+      elements4(x[i], j, T{}, y);
+      if (quick) {
+        w[j] = encode4<TYPE>(y, s, rcp);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = C::quotient(y[e], s, rcp, any_scale);
+        w[j] = C::pack4(y);
+      }
+    }
+    uint8_t* dst = codes + (size_t)row * D + at;
+    if constexpr (kEl == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = w[0];
   }
 }
 

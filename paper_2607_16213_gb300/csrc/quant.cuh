@@ -153,12 +153,25 @@ cudaError_t launch_qread(const QReadArgs& a, cudaStream_t s);
 // Decode over an 8-bit cache: DecodeArgs without Kc and Vc.
 struct QDecodeArgs : DecodeArgs {
   QCache c;
-  uint32_t* cnt_kv;  // [B][Hkv] units of a KV head that are done (self-resetting)
+  int warps;
+  int cluster;  // CTAs of a cluster: 1, 2, 4 or 8; divides the splits
 };
-// Units of a KV head: its query heads that one CTA takes together.
-int decode_q_units(int dtype, int G);
-int decode_q_splits(const selkv_shape& s);
+// Warps of a CTA and splits of a (sequence, KV head)'s rows.
+struct QDecodePlan {
+  int warps, splits, cluster;
+};
+QDecodePlan decode_q_plan(const selkv_shape& s);
+// CTA sizes: few (sequence, KV head) pairs get large CTAs, one on an SM (few splits to fold); many get
+// small ones.
+constexpr int ctas_of(int warps, bool wide) { return warps == 8 ? (wide ? 1 : 2) : wide ? 2 : 4; }  // CTAs on an SM
+constexpr int kMaxSplits = kPlanSMs;
+// Floats of a (sequence, KV head)'s record of partials, where there are several clusters (Sg).
+__host__ __device__ constexpr size_t decode_q_record_floats(int G, int Sc, int Sg, int D) {
+  return (size_t)G * Sg * D + (((size_t)Sc * G * Sg * 2 + 3) & ~(size_t)3);
+}
 cudaError_t launch_decode_q(const QDecodeArgs& a, cudaStream_t s);
+cudaError_t launch_decode_q_e4m3(const QDecodeArgs& a, cudaStream_t s);
+cudaError_t launch_decode_q_int8(const QDecodeArgs& a, cudaStream_t s);
 
 // One lane's elements of a row of D, as fp32, by a whole warp: lane l holds l * D / 32 onwards.
 template <typename T, int D>
