@@ -127,7 +127,7 @@ def _bad(what: str) -> None:
 
 
 def _tensor(t: torch.Tensor, name: str, shape, dtype, device) -> None:
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device.index or not t.is_contiguous():
         _bad("%s: a contiguous %s tensor %s on %s is wanted, not %s %s on %s"
              % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
@@ -190,20 +190,16 @@ def alloc_quant(shape: B.selkv_shape, cache_type: str = "e4m3", block: int = 64,
 _raw_stream = torch._C._cuda_getCurrentRawStream  # (current_stream() builds an object: 2.9 us a call against 0.2)
 
 
+def _elsewhere(device: torch.device, stream) -> bool:
+    return stream is not None or torch.cuda.current_device() != device.index
+
+
 @contextlib.contextmanager
-def _switched(device: torch.device, stream):
-    with torch.cuda.device(device):
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-        with torch.cuda.stream(s):  # (None: nothing changes)
-            yield s.cuda_stream if s is not None else _raw_stream(device.index)
-
-
 def _on(device: torch.device, stream):
-    """Context with the cache's device current, and allocations made on the stream that the call runs
-    on; its value is that stream."""
-    if stream is None and torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext(_raw_stream(device.index))
-    return _switched(device, stream)
+    """The cache's device current, and allocations made on the stream that the call runs on."""
+    with torch.cuda.device(device):
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            yield
 
 
 def quant_append(cache: QuantCache, K_new: torch.Tensor, V_new: torch.Tensor, bias_new: Optional[torch.Tensor] = None,
@@ -211,6 +207,10 @@ def quant_append(cache: QuantCache, K_new: torch.Tensor, V_new: torch.Tensor, bi
     """selkv_qcache_append: rows [B][Hkv][T][d] (the first counts[b] of each sequence) behind those of
     the cache, in place."""
     s, dev = cache.shape, cache.K.device
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return quant_append(cache, K_new, V_new, bias_new, counts, workspace)
+    st = _raw_stream(dev.index)
     T = K_new.shape[2] if K_new.dim() == 4 else 0
     want = (s.batch, s.num_kv_heads, T, s.head_dim)
     _tensor(K_new, "quant_append: K_new", want, cache._dtype, dev)
@@ -219,19 +219,21 @@ def quant_append(cache: QuantCache, K_new: torch.Tensor, V_new: torch.Tensor, bi
         _tensor(bias_new, "quant_append: bias_new", want[:3], torch.float32, dev)
     if counts is not None:
         _tensor(counts, "quant_append: counts", (s.batch,), torch.int32, dev)
-    with _on(dev, stream) as st:
-        ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
-        B.check(B.selkv_qcache_append(s, cache._bias, T, K_new, V_new, bias_new, counts, ws.buf, ws.nbytes, st),
-                "selkv_qcache_append")
+    ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+    B.check(B.selkv_qcache_append(s, cache._bias, T, K_new, V_new, bias_new, counts, ws.buf, ws.nbytes, st),
+            "selkv_qcache_append")
     return cache
 
 
 def quantize(cache: CompressedCache, cache_type: str = "e4m3", block: int = 64, workspace: Optional[Workspace] = None,
              stream=None) -> QuantCache:
     """The compressed cache in 8 bits: its rows, compensation and lengths in a QuantCache of its capacity."""
-    with _on(cache.K_c.device, stream) as st:
-        q = alloc_quant(cache.shape, cache_type, block, True, cache.K_c.device)
-        return quant_append(q, cache.K_c, cache.V_c, cache.bias, cache.lengths[:cache.shape.batch], workspace, st)
+    dev = cache.K_c.device
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return quantize(cache, cache_type, block, workspace)
+    q = alloc_quant(cache.shape, cache_type, block, True, dev)
+    return quant_append(q, cache.K_c, cache.V_c, cache.bias, cache.lengths[:cache.shape.batch], workspace)
 
 
 def quant_read(cache: QuantCache, row0: int = 0, rows: Optional[int] = None, out=None,
@@ -239,19 +241,22 @@ def quant_read(cache: QuantCache, row0: int = 0, rows: Optional[int] = None, out
     """selkv_qcache_read: (K, V) of rows row0 .. row0 + rows - 1, [B][Hkv][rows][d] (with `out` given its
     rows behind the lengths stay, else they are zeros)."""
     s, dev = cache.shape, cache.K.device
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return quant_read(cache, row0, rows, out, workspace)
+    st = _raw_stream(dev.index)
     if rows is None:
         rows = out[0].shape[2] if out is not None else s.m_cap - row0
     want = (s.batch, s.num_kv_heads, rows, s.head_dim)
-    with _on(dev, stream) as st:
-        if out is None:
-            if rows < 1:
-                _bad("quant_read: rows")
-            out = tuple(torch.zeros(want, dtype=cache._dtype, device=dev) for _ in range(2))
-        K, V = out
-        _tensor(K, "quant_read: K", want, cache._dtype, dev)
-        _tensor(V, "quant_read: V", want, cache._dtype, dev)
-        ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
-        B.check(B.selkv_qcache_read(s, cache._bias, row0, rows, K, V, ws.buf, ws.nbytes, st), "selkv_qcache_read")
+    if out is None:
+        if rows < 1:
+            _bad("quant_read: rows")
+        out = tuple(torch.zeros(want, dtype=cache._dtype, device=dev) for _ in range(2))
+    K, V = out
+    _tensor(K, "quant_read: K", want, cache._dtype, dev)
+    _tensor(V, "quant_read: V", want, cache._dtype, dev)
+    ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+    B.check(B.selkv_qcache_read(s, cache._bias, row0, rows, K, V, ws.buf, ws.nbytes, st), "selkv_qcache_read")
     return K, V
 
 
@@ -261,18 +266,21 @@ def decode_quant(cache: QuantCache, q: torch.Tensor, k_new: Optional[torch.Tenso
     """selkv_decode_attn_q: one token [B][Hq][d] over an 8-bit cache (optionally appending k_new / v_new
     [B][Hkv][d])."""
     s, dev = cache.shape, cache.K.device
-    want = (s.batch, s.num_q_heads, s.head_dim)
-    _tensor(q, "decode_quant: q", want, cache._dtype, dev)
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return decode_quant(cache, q, k_new, v_new, use_bias, out, workspace)
+    st = _raw_stream(dev.index)
+    want, dt = (s.batch, s.num_q_heads, s.head_dim), cache._dtype
+    _tensor(q, "decode_quant: q", want, dt, dev)
     if k_new is not None and v_new is not None:
         new = (s.batch, s.num_kv_heads, s.head_dim)
-        _tensor(k_new, "decode_quant: k_new", new, cache._dtype, dev)
-        _tensor(v_new, "decode_quant: v_new", new, cache._dtype, dev)
-    with _on(dev, stream) as st:
-        if out is None:
-            out = torch.empty_like(q)
-        else:
-            _tensor(out, "decode_quant: out", want, cache._dtype, dev)
-        ws = workspace or Workspace(B.selkv_decode_q_workspace_size(s), dev, st)
-        B.check(B.selkv_decode_attn_q(s, cache._bias if use_bias else cache._plain, q, k_new, v_new, out, ws.buf,
-                                      ws.nbytes, st), "selkv_decode_attn_q")
+        _tensor(k_new, "decode_quant: k_new", new, dt, dev)
+        _tensor(v_new, "decode_quant: v_new", new, dt, dev)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _tensor(out, "decode_quant: out", want, dt, dev)
+    ws = workspace or Workspace(B.selkv_decode_q_workspace_size(s), dev, st)
+    B.check(B.selkv_decode_attn_q(s, cache._bias if use_bias else cache._plain, q, k_new, v_new, out, ws.buf, ws.nbytes, st),
+            "selkv_decode_attn_q")
     return out

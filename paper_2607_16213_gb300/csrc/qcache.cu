@@ -9,7 +9,17 @@
 namespace selkv {
 namespace {
 
-constexpr int kTileRows = 128, kWarpRows = 16, kAppendThreads = 256;
+constexpr int kTileRows = 128;
+// Rows of a warp: at most 32 registers of elements a lane, and no more than the smallest block.  CTAs of a tile on an
+// SM: as many as registers hold (25000 x 8 rows of bf16, d 128: two or three CTAs 33.9 us, four 30.8,
+// five 29.7, six 35.5).
+template <typename T, int D>
+struct ACfg {
+  static constexpr bool kLight = D * sizeof(T) == 128;
+  static constexpr int kWarpRows = D * sizeof(T) == 512 ? 8 : 16;
+  static constexpr int kThreads = kTileRows / kWarpRows * 32;
+  static constexpr int kCtas = (kLight ? 2048 : 1280) / kThreads;
+};
 
 // Four consecutive elements of 16 loaded bytes.
 __device__ __forceinline__ void elements4(const uint4& w, int half, __nv_bfloat16, float (&x)[4]) {
@@ -54,26 +64,34 @@ __device__ __forceinline__ uint32_t max_finite_bits(const uint4 (&w)[N]) {
     }
   return __float_as_uint(m);
 }
-// Four finite bf16 elements as codes under a scale of the grid.
-template <int TYPE>
+// Four finite elements as codes under a scale of the grid.  For int8 the integer is in the low bits of
+// quotient + 1.5 * 2^23; for fp32 elements it is then checked against the remainder.
+template <int TYPE, typename T>
 __device__ __forceinline__ uint32_t encode4(const float (&x)[4], float s, float rcp) {
   if constexpr (TYPE == SELKV_Q_E4M3) {
     return cvt_e4m3x2(x[0] * rcp, x[1] * rcp) | cvt_e4m3x2(x[2] * rcp, x[3] * rcp) << 16;
   } else {
-    // the integer nearest to the quotient is in the low bits of quotient + 1.5 * 2^23
+    constexpr float kBig = 12582912.f;
     uint32_t t[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float q = x[e] * rcp;
-      t[e] = __float_as_uint(fmaf(fmaf(-q, s, x[e]), rcp, q) + 12582912.f);
+      if constexpr (sizeof(T) == 2) {
+        t[e] = __float_as_uint(fmaf(fmaf(-q, s, x[e]), rcp, q) + kBig);
+      } else {
+        const float c = q + kBig, r = fmaf(-(c - kBig), s, x[e]), h = 0.5f * s;
+        const bool off = fabsf(r) > h || (fabsf(r) == h && (__float_as_uint(c) & 1u));
+        t[e] = __float_as_uint(off ? c + copysignf(1.f, r) : c);
+      }
     }
     return __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
   }
 }
 
 template <int TYPE, typename T, int D>
-__global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) {
+__global__ __launch_bounds__(ACfg<T, D>::kThreads, ACfg<T, D>::kCtas) void qappend_kernel(QAppendArgs a) {
   using C = Code<TYPE>;
+  constexpr int kWarpRows = ACfg<T, D>::kWarpRows, kThreads = ACfg<T, D>::kThreads;
   constexpr int kEl = 16 / sizeof(T);           // elements of a 16-byte load
   constexpr int kLpr = D / kEl;                 // lanes per row
   constexpr int kRpl = 32 / kLpr;               // rows per load
@@ -106,7 +124,7 @@ __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) 
     x[i] = row >= L && row < L + n ? *reinterpret_cast<const uint4*>(src + (size_t)(row - L) * D + at) : make_uint4(0, 0, 0, 0);
   }
   // The last CTA of the sequence to have read its length moves it: every one has read it by then.
-  if (tid == kAppendThreads - 1) {
+  if (tid == kThreads - 1) {
     const uint32_t all = gridDim.x * gridDim.y * 2u;
     if (atom_add_acq_rel_gpu(&a.cnt_seq[b], 1u) == all - 1u) {
       a.cnt_seq[b] = 0u;
@@ -151,7 +169,7 @@ __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) 
     }
   }
   const float rcp = 1.f / s;
-  const bool any_scale = holds || sizeof(T) == 4, quick = finite && !any_scale;
+  const bool quick = finite && !holds;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int row = row0 + i * kRpl + lane / kLpr;
@@ -162,10 +180,10 @@ __global__ __launch_bounds__(kAppendThreads) void qappend_kernel(QAppendArgs a) 
       float y[4];
       elements4(x[i], j, T{}, y);
       if (quick) {
-        w[j] = encode4<TYPE>(y, s, rcp);
+        w[j] = encode4<TYPE, T>(y, s, rcp);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = C::quotient(y[e], s, rcp, any_scale);
+        for (int e = 0; e < 4; ++e) y[e] = C::quotient(y[e], s, rcp, holds || sizeof(T) == 4);
         w[j] = C::pack4(y);
       }
     }
@@ -227,8 +245,8 @@ template <int TYPE, typename T>
 cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
   // the rows behind any length touch at most this many tiles
   const dim3 grid((a.rows + kTileRows - 2) / kTileRows + 1, a.Hkv, 2 * a.B);
-  if (a.D == 128) qappend_kernel<TYPE, T, 128><<<grid, kAppendThreads, 0, st>>>(a);
-  else qappend_kernel<TYPE, T, 64><<<grid, kAppendThreads, 0, st>>>(a);
+  if (a.D == 128) qappend_kernel<TYPE, T, 128><<<grid, ACfg<T, 128>::kThreads, 0, st>>>(a);
+  else qappend_kernel<TYPE, T, 64><<<grid, ACfg<T, 64>::kThreads, 0, st>>>(a);
   return cudaGetLastError();
 }
 
