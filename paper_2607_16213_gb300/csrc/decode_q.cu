@@ -19,7 +19,8 @@ namespace selkv {
 //   256 x 2      one split: 4.9, two: 5.9
 // Clusters of more than 64 CTAs in all are placed two CTAs to an SM although others are free (25000 x 16
 // as clusters of 8: 29 us, split through memory 24), and larger ones than 8 are not placed everywhere.
-QDecodePlan decode_q_plan(const selkv_shape& s) {
+namespace {
+QDecodePlan plan_of(const selkv_shape& s) {
   const long n = (long)s.batch * s.num_kv_heads, rows = s.m_cap;
   const bool wide = s.num_q_heads / s.num_kv_heads > 8 || s.dtype == SELKV_FP32;
   const int warps = n >= kPlanSMs / 2 ? 4 : 8;
@@ -50,6 +51,19 @@ QDecodePlan decode_q_plan(const selkv_shape& s) {
     }
   }
   return best;
+}
+}  // namespace
+
+// (The search takes some microseconds; a decode comes back with the same shape call after call.)
+QDecodePlan decode_q_plan(const selkv_shape& s) {
+  static thread_local selkv_shape of{};
+  static thread_local QDecodePlan plan{};
+  if (plan.warps == 0 || of.dtype != s.dtype || of.batch != s.batch || of.num_q_heads != s.num_q_heads ||
+      of.num_kv_heads != s.num_kv_heads || of.head_dim != s.head_dim || of.m_cap != s.m_cap) {
+    plan = plan_of(s);
+    of = s;
+  }
+  return plan;
 }
 
 cudaError_t launch_decode_q(const QDecodeArgs& a, cudaStream_t st) {

@@ -33,14 +33,13 @@ constexpr int kTileRows = 32;  // rows of a warp's tile: one bias a lane
 template <int D, int NT, int NW>
 struct QCfg {
   static constexpr int kWarps = NW, kThreads = NW * 32;
-  static constexpr int kSlots = 2;  // K or V tiles in flight per warp
   static constexpr int kSlot = kTileRows * D;
   static constexpr int kFoldLd = D + 4;               // fold row stride (floats): conflict-free float2 stores
   static constexpr int kFold = NW * 8 * NT * kFoldLd * 4;
   static constexpr int kPart = 8 * NT * D * 4;         // a cluster's CTA: its folded output
-  static constexpr int kTiles = NW * kSlots * kSlot;  // the rings, and the fold in their place
+  static constexpr int kTiles = NW * 2 * kSlot;  // the rings, and the fold in their place
   static constexpr int kRing = kTiles > kFold + kPart ? kTiles : kFold + kPart;
-  static constexpr int kSmem = 1024 + kRing + kWarps * kSlots * 8;
+  static constexpr int kSmem = 1024 + kRing + kWarps * 2 * 8;
 };
 
 // Byte offset of 16-byte chunk c of row r in a tile written by TMA with 128-byte (D = 128) or
@@ -127,20 +126,20 @@ template <int TYPE, typename T, int D, int NT, int NW>
 __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) void decode_q_kernel(
     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, QDecodeArgs a) {
   using C = QCfg<D, NT, NW>;
-  constexpr int kWarps = C::kWarps, kSlots = C::kSlots, kThreads = C::kThreads;
+  constexpr int kWarps = C::kWarps, kThreads = C::kThreads;
   constexpr int NC = D / 16;                    // 16-byte chunks of a code row
   constexpr int NP = sizeof(T) == 4 ? 2 : 1;    // halves of a query or weight
   constexpr int GU = 8 * NT;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kRing);  // [kWarps][kSlots]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kRing);  // [kWarps][2]
   __shared__ float wm[kWarps][GU], wl[kWarps][GU];
   __shared__ float apm[GU], s_M[GU];  // the appended row's logits; the largest logits
   __shared__ float s_inv[GU];
   __shared__ __align__(16) float s_vnew[D];  // the appended row's values
   __shared__ float2 s_ml[GU];  // (largest logit, sum) of the CTA's rows
-  __shared__ int s_abort;
+  __shared__ int s_abort, s_len;
   __shared__ bool s_last;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -149,11 +148,10 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
   // split s: CTA `rank` of `Sc` in cluster `sg` of `Sg`
   const int Sc = a.cluster, Sg = S / Sc, rank = s % Sc, sg = s / Sc;
   const size_t bk = (size_t)b * a.Hkv + kv, bh0 = bk * G;
-  uint64_t* bar = full + warp * kSlots;
-  unsigned char* ring = smem + warp * kSlots * C::kSlot;
+  uint64_t* bar = full + warp * 2;
 
   if (lane == 0) {
-    for (int i = 0; i < kSlots; ++i) mbar_init(&bar[i], 1);
+    for (int i = 0; i < 2; ++i) mbar_init(&bar[i], 1);
     fence_mbar_init();
     if (warp == 0) {
       s_abort = 0;
@@ -161,7 +159,6 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
       prefetch_tensormap(&tmV);
     }
   }
-  __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
 
@@ -169,7 +166,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
   // slice is known, the first tile's scales are asked for before the tiles: behind those they would
   // wait for the whole ring (25000 rows x 8 heads: queries there after 5.1 us instead of 1.7).
   const int g = lane >> 2, j = lane & 3;
-  int L = a.lengths[b];
+  if (tid == kThreads - 1) s_len = a.lengths[b];  // (the CTA's only thread to read it)
   Row4<T> qr[NT][NC];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -181,6 +178,8 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
     if (lane < 2 * kLines)
       prefetch_l2(static_cast<const char*>(lane < kLines ? a.k_new : a.v_new) + bk * D * sizeof(T) + lane % kLines * 128);
   }
+  __syncthreads();
+  int L = s_len;
   if (L < 0 || L > a.m_cap) {
     if (tid == 0 && s == 0 && kv == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
     L = L < 0 ? 0 : a.m_cap;
@@ -196,32 +195,42 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
   const int lo = min(L, s * chunk), hi = min(L, lo + chunk);
   const int ntiles = (hi - lo + kTileRows - 1) / kTileRows;
   const int nt = warp < ntiles ? (ntiles - warp + kWarps - 1) / kWarps : 0;  // this warp's
-  // the warp's stream of tiles: K of its tile i is item 2 i, V item 2 i + 1, each in slot item % kSlots
-  auto issue = [&](int item) {  // (lane 0)
-    const int st = item % kSlots, y = (int)(bk * a.m_cap) + lo + (warp + (item >> 1) * kWarps) * kTileRows;
-    mbar_arrive_expect_tx(&bar[st], C::kSlot);
-    tma_load_2d(ring + st * C::kSlot, item & 1 ? &tmV : &tmK, 0, y, &bar[st]);
+  // the warp's tiles: i is rows row0 + i * kStep .. + 31; K in slot 0 of its ring, V in slot 1
+  constexpr int kStep = kWarps * kTileRows;
+  const int row0 = lo + warp * kTileRows, y0 = (int)(bk * a.m_cap) + row0;
+  unsigned char *ring_k = smem + warp * 2 * C::kSlot, *ring_v = ring_k + C::kSlot;
+  auto issue_k = [&](int i) {  // (lane 0)
+    mbar_arrive_expect_tx(&bar[0], C::kSlot);
+    tma_load_2d(ring_k, &tmK, 0, y0 + i * kStep, &bar[0]);
   };
-  const float* brow = a.bias != nullptr ? a.bias + bk * a.m_cap : nullptr;
+  auto issue_v = [&](int i) {
+    mbar_arrive_expect_tx(&bar[1], C::kSlot);
+    tma_load_2d(ring_v, &tmV, 0, y0 + i * kStep, &bar[1]);
+  };
   float* ksp = a.c.ks + bk * a.c.nblk;
   float* vsp = a.c.vs + bk * a.c.nblk;
-  // bias (of row `lane`; -inf: no weight) and scales (of each half) of a tile, fetched one tile ahead
+  // Bias (of row `lane`; -inf: no weight) and scales (of each half) of a tile, fetched one tile ahead.  A step
+  // is a whole number of blocks, so that all of them are a fixed way from the tile before.
   struct Side {
     float bias, ks[2], vs[2];
   };
   const bool halves = a.c.block_log2 == 4;  // a tile's halves have scales of their own
-  auto fetch = [&](int i) {
-    Side f;
-    const int row = lo + (warp + i * kWarps) * kTileRows;
-    f.bias = row + lane < hi ? (brow != nullptr ? brow[row + lane] : 0.f) : -INFINITY;
-    int blk = row >> a.c.block_log2;
-    f.ks[0] = f.ks[1] = ksp[blk];
-    f.vs[0] = f.vs[1] = vsp[blk];
-    if (halves && row + 16 < hi) {
-      f.ks[1] = ksp[blk + 1];
-      f.vs[1] = vsp[blk + 1];
+  const int blk0 = row0 >> a.c.block_log2, blk_step = kStep >> a.c.block_log2;
+  const float *bias_at = a.bias != nullptr ? a.bias + bk * a.m_cap + row0 + lane : nullptr;
+  const float *ks_at = ksp + blk0, *vs_at = vsp + blk0;
+  int left = hi - row0;  // rows of the slice from the tile on
+  auto fetch = [&](Side& f) {
+    f.bias = lane < left ? (bias_at != nullptr ? *bias_at : 0.f) : -INFINITY;
+    f.ks[0] = f.ks[1] = *ks_at;
+    f.vs[0] = f.vs[1] = *vs_at;
+    if (halves && left > 16) {
+      f.ks[1] = ks_at[1];
+      f.vs[1] = vs_at[1];
     }
-    return f;
+    if (bias_at != nullptr) bias_at += kStep;
+    ks_at += blk_step;
+    vs_at += blk_step;
+    left -= kStep;
   };
   // the appended row joins the split that reads its block
   const bool joins = app && s == (L > 0 ? (L - 1) / chunk : 0);
@@ -231,9 +240,11 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
     if (tid < D) vn = load1(static_cast<const T*>(a.v_new) + bk * D + tid);
   }
   Side next{};
-  if (nt > 0) next = fetch(0);
-  if (lane == 0)
-    for (int i = 0; i < min(2 * nt, kSlots); ++i) issue(i);
+  if (nt > 0) fetch(next);
+  if (lane == 0 && nt > 0) {
+    issue_k(0);
+    issue_v(0);
+  }
 
   // The last CTA of the sequence to have read its length moves it (while the first tiles are on their way).
   if (app && tid == kThreads - 1 && atom_add_acq_rel_gpu(&a.cnt_seq[b], 1u) == (uint32_t)(S * a.Hkv) - 1u) {
@@ -301,19 +312,18 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
     }
   }
 
-  int done = 0;
+  int got_k = 0, got_v = 0;  // tiles read
   for (int i = 0; i < nt; ++i) {
     const Side cur = next;
-    if (i + 1 < nt) next = fetch(i + 1);
-    const int sk = (2 * i) % kSlots, sv = (2 * i + 1) % kSlots;
-    if (!__all_sync(0xffffffffu, mbar_wait(&bar[sk], ((2 * i) / kSlots) & 1))) {
+    if (i + 1 < nt) fetch(next);
+    if (!__all_sync(0xffffffffu, mbar_wait(&bar[0], i & 1))) {
       if (lane == 0) {
         s_abort = 1;
         raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
       }
       break;
     }
-    const uint32_t Kt = smem_u32(ring + sk * C::kSlot), Vt = smem_u32(ring + sv * C::kSlot);
+    const uint32_t Kt = smem_u32(ring_k), Vt = smem_u32(ring_v);
     const float bl = bias_log2(cur.bias);
     const uint32_t dead = __ballot_sync(0xffffffffu, bl == -INFINITY);
     // S^T = K Q^T: the bytes 4 j .. 4 j + 3 of chunk c are the k indexes 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of step c
@@ -339,9 +349,9 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
           for (int p = 0; p < NP; ++p) mma_f16_16816(x[n][h], ka, qb[n][p][c]);
       }
     }
-    done = 2 * i + 1;
+    got_k = i + 1;
     __syncwarp();
-    if (lane == 0 && done - 1 + kSlots < 2 * nt) issue(done - 1 + kSlots);
+    if (lane == 0 && i + 1 < nt) issue_k(i + 1);
     // logits in base 2
     float tm[NT][2];
 #pragma unroll
@@ -429,7 +439,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
           pb[n][0][h][q] = transpose8(w);
           if constexpr (NP == 2) pb[n][NP - 1][h][q] = transpose8(pack_rest(p0, p1, w));
         }
-    if (!__all_sync(0xffffffffu, mbar_wait(&bar[sv], ((2 * i + 1) / kSlots) & 1))) {
+    if (!__all_sync(0xffffffffu, mbar_wait(&bar[1], i & 1))) {
       if (lane == 0) {
         s_abort = 1;
         raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
@@ -441,7 +451,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
       for (uint32_t rest = dead; rest != 0; rest &= rest - 1) {
         const int r = __ffs(rest) - 1;
         if (lane < NC)
-          *reinterpret_cast<uint4*>(ring + sv * C::kSlot + tile_at<D>(r, lane)) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(ring_v + tile_at<D>(r, lane)) = make_uint4(0, 0, 0, 0);
       }
       __syncwarp();
     }
@@ -466,11 +476,13 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
       }
     if (dead) fence_proxy_async_smem();
     __syncwarp();
-    done = 2 * i + 2;
-    if (lane == 0 && done - 1 + kSlots < 2 * nt) issue(done - 1 + kSlots);
+    got_v = i + 1;
+    if (lane == 0 && i + 1 < nt) issue_v(i + 1);
   }
-  // every copy has landed before the ring is used again or the CTA leaves
-  for (int i = done; i < min(2 * nt, done + kSlots); ++i) mbar_wait(&bar[i % kSlots], (i / kSlots) & 1);
+  // every copy has landed before the ring is used again or the CTA leaves (tile i's K is asked for when that
+  // of i - 1 has been read)
+  if (got_k < nt) mbar_wait(&bar[0], got_k & 1);
+  if (got_v < nt) mbar_wait(&bar[1], got_v & 1);
 
   // Fold of the warps, the lanes' sums of a head first.
 #pragma unroll

@@ -100,7 +100,13 @@ __global__ __launch_bounds__(ACfg<T, D>::kThreads, ACfg<T, D>::kCtas) void qappe
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
   const size_t bk = (size_t)b * a.Hkv + h;
-  int L = a.c.lengths[b], n = a.counts != nullptr ? a.counts[b] : a.rows;
+  __shared__ int s_len, s_n;
+  if (tid == kThreads - 1) {  // (the CTA's only thread to read the length)
+    s_len = a.c.lengths[b];
+    s_n = a.counts != nullptr ? a.counts[b] : a.rows;
+  }
+  __syncthreads();
+  int L = s_len, n = s_n;
   const bool first_cta = blockIdx.x == 0 && h == 0 && isv == 0;
   if (L < 0 || L > a.m_cap || n < 0 || n > a.rows) {
     if (tid == 0 && first_cta) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
@@ -123,7 +129,8 @@ __global__ __launch_bounds__(ACfg<T, D>::kThreads, ACfg<T, D>::kCtas) void qappe
     const int row = row0 + i * kRpl + lane / kLpr;
     x[i] = row >= L && row < L + n ? *reinterpret_cast<const uint4*>(src + (size_t)(row - L) * D + at) : make_uint4(0, 0, 0, 0);
   }
-  // The last CTA of the sequence to have read its length moves it: every one has read it by then.
+  // The last CTA of the sequence to have read its length moves it.  (Behind the loads: the thread waits for the
+  // counter, and its warp with it.)
   if (tid == kThreads - 1) {
     const uint32_t all = gridDim.x * gridDim.y * 2u;
     if (atom_add_acq_rel_gpu(&a.cnt_seq[b], 1u) == all - 1u) {
