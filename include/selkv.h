@@ -404,7 +404,8 @@ SELKV_API selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv
 /* Rows back out of the cache: rows row0 .. row0 + rows - 1 of each (b, kv) that lie below lengths[b], as
  * code * scale rounded once to the shape's dtype, into K_out and V_out [B][Hkv][rows][d].  Rows at
  * or behind lengths[b] of the outputs are left as they were.  0 <= row0, 1 <= rows,
- * row0 + rows <= m_cap.  Errors as above. */
+ * row0 + rows <= m_cap.  The outputs may be K_c and V_c of a selkv_decode_attn that follows at once (the
+ * one exception to "Overlap with the previous kernel").  Errors as above. */
 SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cache, int32_t row0,
                                          int32_t rows, void* K_out, void* V_out, void* workspace,
                                          size_t workspace_bytes, selkv_stream_t stream);
@@ -417,8 +418,8 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * + 1), all inside the call.
  *
  * q, out        [B][Hq][d] of the shape's dtype; k_new, v_new [B][Hkv][d] or both NULL.
- * A row whose bias is -inf has no weight, and a head whose rows all have none gives out = 0, as
- * does an empty cache without a new row; rows whose bias is the lowest finite number are the limit of very
+ * A row whose bias is -inf has no weight, whatever its codes, and a head whose rows all have none
+ * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite number are the limit of very
  * small weights (rows that all have it share the weight).  An append that would pass m_cap is
  * skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
  * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */

@@ -5,7 +5,10 @@
 // with codes kc, vc of 8 bits and scales ks, vs of a block of rows.  Split-K flash decoding: CTA (split,
 // KV head, sequence) takes a contiguous slice of the rows, cut at multiples of 64.  Each of its warps is
 // a stream of its own: it takes every kWarps-th tile of 32 rows, which its lane 0 brings into the warp's own
-// ring of shared memory with two 2D TMA loads (K and V), so no warp waits for another in the loop.
+// shared memory with two 2D TMA loads (K and V; the next K as soon as this one is multiplied, the next V
+// likewise), so no warp waits for another in the loop.  64 KB in flight on an SM is as much as helps:
+// with 128 KB one token over 131072 x 8 rows takes 45.5 us instead of 44.6, with 192 KB 49.8, as whatever is
+// asked for queues behind it.
 //
 // Per tile S^T = K Q^T and O^T += V^T P^T run on the tensor cores (mma.sync m16n8k16): the rows and the
 // elements of the cache are the 16 of the product and the heads of a group its 8 (one step for up to
@@ -13,13 +16,16 @@
 // tcgen05 tile, and its codes have to pass through registers to become fp16.
 //
 // Numbers.  A code is exact in fp16.  A query row is scaled by a power of two to a largest magnitude in [2^14, 2^15)
-// and held in fp16: exactly for bf16; an fp32 query as the sum of two halves (22 bits).  A tile's
-// weights p = 2^(x - largest x of the tile) are summed in fp32, and go into O as
-//   fp16(p * vs * 2^(largest x - ref)),
+// and held in fp16: exactly for bf16; an fp32 query as the sum of two halves (22 bits).  The
+// weights p = 2^(x - largest x so far) are summed in fp32, and go into O as
+//   fp16(p * vs * 2^(largest x so far - ref)),
 // ref a reference that only grows and keeps these below 2^15: the scales of V never meet O, and
 // weights down to 2^-24 of the largest keep 11 bits (fp32 caches: 22, as two halves).
 //
-// A key row costs 2 d + 4 bytes of HBM and 4 G d flops.
+// A key row costs 2 d + 4 bytes of HBM and 4 G d flops.  What bounds it: HBM from some tens of MB on
+// (131072 x 8 rows of d 128, 269 MB: 44.6 us, 6.0 TB/s of 6.8 measured for a copy); below that the way in
+// (length, queries and the first tiles: 3 us) and out (fold of warps and splits: 2 to 4 us); for d 64
+// the work of a tile, which is that of d 128 but for half of the products.
 #pragma once
 
 #include "decode_common.cuh"
@@ -133,7 +139,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kRing);  // [kWarps][2]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kRing);  // [kWarps][K, V]
   __shared__ float wm[kWarps][GU], wl[kWarps][GU];
   __shared__ float apm[GU], s_M[GU];  // the appended row's logits; the largest logits
   __shared__ float s_inv[GU];

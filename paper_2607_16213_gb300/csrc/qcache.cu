@@ -213,7 +213,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-constexpr int kReadThreads = 256;
+constexpr int kReadThreads = 128, kReadLoads = 2;
 
 template <int TYPE, typename T, int D>
 __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
@@ -225,27 +225,42 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && isv == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
     L = min(max(L, 0), a.m_cap);
   }
-  const int n = min(a.rows, L - a.row0);  // rows to read (none: <= 0)
+  const int n = max(0, min(a.rows, L - a.row0));  // rows to read
   const uint8_t* codes = (isv ? a.c.V : a.c.K) + (bk * a.m_cap + a.row0) * D;
   const float* scales = (isv ? a.c.vs : a.c.ks) + bk * a.c.nblk;
   T* out = static_cast<T*>(isv ? a.v_out : a.k_out) + bk * a.rows * D;
-  const int i = blockIdx.x * kReadThreads + threadIdx.x;  // 16 codes each
-  const int row = i / (D / 16);
-  if (row >= n) return;
-  const uint4 w = *reinterpret_cast<const uint4*>(codes + (size_t)i * 16);
-  const float s = scales[(a.row0 + row) >> a.c.block_log2];
-  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  const int i0 = blockIdx.x * (kReadThreads * kReadLoads) + threadIdx.x;  // 16 codes each
+  if (blockIdx.x * (kReadThreads * kReadLoads) / (D / 16) >= n) return;
+  uint4 w[kReadLoads];
+  float s[kReadLoads];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    float y[8], t[4];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      C::unpack4(ws[j * 2 + p], t);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[p * 4 + e] = t[e] * s;
-    }
-    store8(out + (size_t)i * 16 + j * 8, y);
+  for (int l = 0; l < kReadLoads; ++l) {
+    const int i = i0 + l * kReadThreads, row = i / (D / 16);
+    if (row >= n) continue;
+    w[l] = *reinterpret_cast<const uint4*>(codes + (size_t)i * 16);
+    s[l] = scales[(a.row0 + row) >> a.c.block_log2];
   }
+#pragma unroll
+  for (int l = 0; l < kReadLoads; ++l) {
+    const int i = i0 + l * kReadThreads;
+    if (i / (D / 16) >= n) continue;
+    const uint32_t ws[4] = {w[l].x, w[l].y, w[l].z, w[l].w};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float y[8], t[4];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        C::unpack4(ws[j * 2 + p], t);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[p * 4 + e] = t[e] * s[l];
+      }
+      store8(out + (size_t)i * 16 + j * 8, y);
+    }
+  }
+  // A decode over the rows may be the next kernel and load some before it waits for this one, once all of its CTAs
+  // have ended: their rows are in place by then.
+  __syncthreads();
+  if (threadIdx.x == 0) __threadfence();
 }
 
 template <int TYPE, typename T>
@@ -259,7 +274,7 @@ cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
 
 template <int TYPE, typename T>
 cudaError_t qread_t(const QReadArgs& a, cudaStream_t st) {
-  const int per = kReadThreads * 16 / a.D;  // rows of a CTA
+  const int per = kReadThreads * kReadLoads * 16 / a.D;  // rows of a CTA
   const dim3 grid((a.rows + per - 1) / per, a.Hkv, 2 * a.B);
   if (a.D == 128) qread_kernel<TYPE, T, 128><<<grid, kReadThreads, 0, st>>>(a);
   else qread_kernel<TYPE, T, 64><<<grid, kReadThreads, 0, st>>>(a);

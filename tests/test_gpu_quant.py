@@ -520,6 +520,36 @@ def test_tokens_in_a_captured_graph_and_on_other_streams():
         assert torch.equal(caches[i].K.view(torch.int8), caches[2 + i].K.view(torch.int8))
 
 
+def test_rows_read_back_are_decoded_over_at_once():
+    """selkv_qcache_read into a bf16 cache and a decode over that cache right behind it, again and again with
+    other rows: the decode sees the rows of its own turn."""
+    B, hq, hkv, d, cap = 1, 32, 8, 128, 9000
+    shape = api.make_shape("bf16", B, hq, hkv, d, 32, cap, cap)
+    g = gen(23)
+    q = torch.randn((B, hq, d), generator=g, device="cuda").bfloat16()
+    caches = []
+    for i in range(3):
+        c = api.alloc_quant(shape, "e4m3", 64)
+        api.quant_append(c, rows(g, B, hkv, cap - i, d, "bf16"), rows(g, B, hkv, cap - i, d, "bf16"))
+        caches.append(c)
+    full = api.alloc_compressed(shape)
+    ws, wr = api.Workspace(S.selkv_decode_workspace_size(shape)), api.Workspace(S.selkv_qcache_workspace_size(shape))
+
+    def one(c, wait):
+        api.quant_read(c, out=(full.K_c, full.V_c), workspace=wr)
+        if wait:
+            torch.cuda.synchronize()
+        return api.decode(full, q, use_bias=False, workspace=ws)
+
+    full.lengths.fill_(cap - 2)
+    want = [one(c, True) for c in caches]
+    assert not torch.equal(want[0], want[1])
+    torch.cuda.synchronize()
+    got = [one(caches[i % 3], False) for i in range(60)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[i], want[i % 3]) for i in range(60))
+
+
 def test_back_to_back_tokens():
     """Many tokens enqueued without a wait between them: each sees all rows before it."""
     B, hq, hkv, d, cap = 2, 8, 2, 128, 700
@@ -541,6 +571,55 @@ def test_back_to_back_tokens():
             check_out(c, model, out[t], q[t], [True] * B, k[t], v[t])
         model.append(k[t][:, :, None], v[t][:, :, None], [1] * B)
     model.check()
+
+
+def test_odd_shapes_of_the_split_rule():
+    """Shapes that the rule splits in each of its ways (one split, a cluster, through memory, both; CTAs of four
+    and eight warps): the outputs agree with the plain form."""
+    for dtype, B, hq, hkv, d, cap, n in (("bf16", 1, 4, 1, 128, 12000, 11990), ("bf16", 1, 16, 1, 128, 9000, 8000), ("fp32", 1, 2, 2, 64, 3001, 3000),
+                                         ("bf16", 9, 32, 8, 64, 700, 650), ("fp32", 20, 16, 4, 128, 500, 499), ("bf16", 3, 16, 16, 128, 900, 77),
+                                         ("bf16", 200, 2, 1, 64, 130, 129), ("bf16", 2, 48, 3, 128, 2600, 2500)):
+        lens = [max(0, n - 37 * i % (n + 1)) for i in range(B)]
+        c, g = filled(dtype, B, hq, hkv, d, cap, "int8" if cap % 2 else "e4m3", 64, lens, cap)
+        model = Model(c)
+        q = torch.randn((B, hq, d), generator=g, device="cuda").to(TORCH[dtype])
+        k, v = (torch.randn((B, hkv, d), generator=g, device="cuda").to(TORCH[dtype]) for _ in range(2))
+        out = api.decode_quant(c, q, k, v)
+        check_out(c, model, out, q, [True] * B, k, v)
+        model.append(k[:, :, None], v[:, :, None], [1] * B)
+        model.check()
+
+
+def test_the_other_sequences_outputs_do_not_depend_on_a_full_one():
+    """A sequence at its capacity among others: it is not appended to, the others are, and its own output is
+    that without a new row."""
+    c, g = filled("bf16", 4, 8, 2, 128, 256, "int8", 32, [256, 10, 255, 0], 31)
+    model = Model(c)
+    q = torch.randn((4, 8, 128), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((4, 2, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    ws = api.Workspace(S.selkv_decode_q_workspace_size(c.shape))
+    for turn in range(3):
+        app = model.L < 256
+        out = api.decode_quant(c, q, k, v, workspace=ws)
+        assert ws.errors() == S.SELKV_DEVERR_CAPACITY
+        check_out(c, model, out, q, app, k, v)
+        model.append(k[:, :, None], v[:, :, None], app.astype(int))
+        model.check()
+
+
+def test_rows_without_weight_may_hold_anything():
+    """Codes that are NaN, under a bias of -inf: in every tile position, for both types of K and V."""
+    B, hq, hkv, d, cap = 2, 8, 2, 128, 600
+    c, g = filled("bf16", B, hq, hkv, d, cap, "e4m3", 32, [590, 95], 41)
+    dead = torch.rand((B, hkv, cap), generator=g, device="cuda") < 0.2
+    c.bias.masked_fill_(dead, -math.inf)
+    for t in (c.K, c.V):
+        t.view(torch.uint8)[dead] = 0x7f
+    model = Model(c)
+    for t in (model.K, model.V):
+        t[np.isnan(t)] = 0.0
+    q = torch.randn((B, hq, d), generator=g, device="cuda").bfloat16()
+    check_out(c, model, api.decode_quant(c, q), q)
 
 
 def test_python_refusals():
