@@ -352,18 +352,19 @@ SELKV_API selkv_status selkv_decode_attn_static(const selkv_shape* shape, const 
  * left (or all rows of an uncompressed cache) in 8 bits an element, with one fp32 scale for each
  * `block` rows of a KV head of K and of V: element = code * scale.
  *
- * Scale and codes of a block, with A the largest finite magnitude of the rows written and qmax the largest
- * code (448 for e4m3, 127 for int8):
+ * Scale and codes of a block, with A the largest finite magnitude of the rows written and qmax the
+ * largest code (448 for e4m3, 127 for int8):
  *   - a block whose first row is written by the call gets the smallest scale s of a grid with
  *     s * qmax >= A, at least 2^-100; the grid is the powers of two for e4m3 and m/8 * 2^e, m = 8..15,
  *     for int8;
  *   - a block that holds rows already keeps its scale s0 times 2^k, with the smallest k >= 0 that
  *     covers A; where k > 0 its old codes become round(code * 2^-k) (exact for e4m3 codes that do
  *     not become subnormal; another rounding of at most half a step for int8);
- *   - a code is the value nearest to element / s, ties to even.  Infinities become +-qmax, a NaN an e4m3 NaN
- *     or the int8 code 0; both set SELKV_DEVERR_VALUE.
- * An element is off by at most s / 2 (int8), or 2^-4 of itself and at least s * 2^-10 (e4m3), and for
- * int8 by up to s / 2 in all further re-encodings.
+ *   - a code is the value nearest to element / s, ties to even.  Infinities become +-qmax, a NaN an
+ *     e4m3 NaN or the int8 code 0; both set SELKV_DEVERR_VALUE.
+ * An element is off by at most s / 2 (int8), or by the larger of 2^-4 of itself and s * 2^-10 (e4m3); where
+ * its block's scale has grown since, an int8 element by less than s of the scale it has now.
+ * (In a partly filled block with a scale of the caller's own the quotient is rounded to fp32 first.)
  * ------------------------------------------------------------------------------------- */
 typedef enum selkv_qtype { SELKV_Q_E4M3 = 0, SELKV_Q_INT8 = 1 } selkv_qtype;
 
@@ -419,9 +420,11 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  *
  * q, out        [B][Hq][d] of the shape's dtype; k_new, v_new [B][Hkv][d] or both NULL.
  * A row whose bias is -inf has no weight, whatever its codes, and a head whose rows all have none
- * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite number are the limit of very
- * small weights (rows that all have it share the weight).  An append that would pass m_cap is
- * skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
+ * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite
+ * number are the limit of very small weights (rows that all have it share the weight).  An append
+ * that would pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
+ * Workspaces: the two kinds are not interchangeable (a decode's is sized for its partials); each is
+ * initialised once with selkv_workspace_init.
  * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */
 SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);
 

@@ -333,7 +333,10 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
     const float bl = bias_log2(cur.bias);
     const uint32_t dead = __ballot_sync(0xffffffffu, bl == -INFINITY);
     // S^T = K Q^T: the bytes 4 j .. 4 j + 3 of chunk c are the k indexes 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of step c
-    float x[NT][2][4];  // heads n * 8 + 2 j + (i & 1), rows 16 h + 8 (i >> 1) + g
+    // (The tensor cores cut sums off instead of rounding them.  With fp32 caches the products with the second halves
+    // of the queries therefore have sums of their own here, and a tile's share of O is added to it below: errors of
+    // 2e-7 to 6e-7 of the output instead of 2e-7 to 1.3e-6.)
+    float x[NT][2][4], x2[NT][2][4] = {};  // heads n * 8 + 2 j + (i & 1), rows 16 h + 8 (i >> 1) + g
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -352,7 +355,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int p = 0; p < NP; ++p) mma_f16_16816(x[n][h], ka, qb[n][p][c]);
+          for (int p = 0; p < NP; ++p) mma_f16_16816(p == 0 ? x[n][h] : x2[n][h], ka, qb[n][p][c]);
       }
     }
     got_k = i + 1;
@@ -372,6 +375,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float& v = x[n][h][q * 2 + e];
+            if constexpr (NP == 2) v += x2[n][h][q * 2 + e];
             v = fmaf(v, qsc[n][e] * cur.ks[h], bv);
             if (dead && bv == -INFINITY) v = bv;  // (the codes may be NaN)
             tm[n][e] = fmaxf(tm[n][e], v);
@@ -475,9 +479,17 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
           to_halves<TYPE, true>(vw[q * 2], va[0], va[1]);
           to_halves<TYPE, true>(vw[q * 2 + 1], va[2], va[3]);
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (NP == 1) {
+              mma_f16_16816(o[n][c + q], va, pb[n][0][h]);
+            } else {
+              float t[4] = {};
+              mma_f16_16816(t, va, pb[n][0][h]);
+              mma_f16_16816(t, va, pb[n][NP - 1][h]);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) mma_f16_16816(o[n][c + q], va, pb[n][p][h]);
+              for (int k = 0; k < 4; ++k) o[n][c + q][k] += t[k];
+            }
+          }
         }
       }
     if (dead) fence_proxy_async_smem();
