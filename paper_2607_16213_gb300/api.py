@@ -127,16 +127,17 @@ def _bad(what: str) -> None:
 
 
 def _tensor(t: torch.Tensor, name: str, shape, dtype, device) -> None:
-    if t.shape != shape or t.dtype != dtype or t.get_device() != device.index or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device.index or not t.is_contiguous():
         _bad("%s: a contiguous %s tensor %s on %s is wanted, not %s %s on %s"
              % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class QuantCache:
     """A cache held in 8 bits (see selkv_qcache in include/selkv.h): codes [B][Hkv][m_cap][d] in
     float8_e4m3fn ("e4m3") or int8 ("int8"), a scale for each `block` rows, compensation per row or
-    None, and the rows held.  Contiguous tensors of one device."""
+    None, and the rows held.  Contiguous tensors of one device, looked over once: they are written in
+    place, not replaced."""
     shape: B.selkv_shape
     cache_type: str
     block: int
@@ -162,9 +163,8 @@ class QuantCache:
                                   ("bias", self.bias, rows, torch.float32), ("lengths", self.lengths, (s.batch,), torch.int32)):
             if t is not None or name != "bias":
                 _tensor(t, "QuantCache." + name, want, dt, dev)
-        self._dtype = _TORCH_DTYPE[s.dtype]
-        self._bias = self._struct(self.bias)
-        self._plain = self._struct(None) if self.bias is not None else self._bias
+        for name, x in (("_dtype", _TORCH_DTYPE[s.dtype]), ("_bias", self._struct(self.bias)), ("_plain", self._struct(None))):
+            object.__setattr__(self, name, x)
 
     def _struct(self, bias) -> B.selkv_qcache:
         return B.selkv_qcache(_QTYPE[self.cache_type], self.block, self.K.data_ptr(), self.V.data_ptr(),
@@ -187,11 +187,12 @@ def alloc_quant(shape: B.selkv_shape, cache_type: str = "e4m3", block: int = 64,
                       torch.zeros((shape.batch,), dtype=torch.int32, device=device))
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # (current_stream() builds an object: 2.9 us a call against 0.2)
+# (torch.cuda.current_stream() builds an object: 2.9 us a call against 0.2)
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _elsewhere(device: torch.device, stream) -> bool:
-    return stream is not None or torch.cuda.current_device() != device.index
+    return stream is not None or _current_device() != device.index
 
 
 @contextlib.contextmanager

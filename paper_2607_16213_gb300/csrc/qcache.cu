@@ -101,6 +101,7 @@ __global__ __launch_bounds__(ACfg<T, D>::kThreads, ACfg<T, D>::kCtas) void qappe
   const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
   const size_t bk = (size_t)b * a.Hkv + h;
   __shared__ int s_len, s_n;
+  chain_begin();
   if (tid == kThreads - 1) {  // (the CTA's only thread to read the length)
     s_len = a.c.lengths[b];
     s_n = a.counts != nullptr ? a.counts[b] : a.rows;
@@ -220,6 +221,7 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
   using C = Code<TYPE>;
   const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
   const size_t bk = (size_t)b * a.Hkv + h;
+  pdl_wait();  // (the next kernel comes up when this one's CTAs have ended: it may load the rows written here)
   int L = a.c.lengths[b];
   if (L < 0 || L > a.m_cap) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && isv == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
@@ -267,18 +269,16 @@ template <int TYPE, typename T>
 cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
   // the rows behind any length touch at most this many tiles
   const dim3 grid((a.rows + kTileRows - 2) / kTileRows + 1, a.Hkv, 2 * a.B);
-  if (a.D == 128) qappend_kernel<TYPE, T, 128><<<grid, ACfg<T, 128>::kThreads, 0, st>>>(a);
-  else qappend_kernel<TYPE, T, 64><<<grid, ACfg<T, 64>::kThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  if (a.D == 128) return launch_chained(true, qappend_kernel<TYPE, T, 128>, grid, dim3(ACfg<T, 128>::kThreads), 0, st, a);
+  return launch_chained(true, qappend_kernel<TYPE, T, 64>, grid, dim3(ACfg<T, 64>::kThreads), 0, st, a);
 }
 
 template <int TYPE, typename T>
 cudaError_t qread_t(const QReadArgs& a, cudaStream_t st) {
   const int per = kReadThreads * kReadLoads * 16 / a.D;  // rows of a CTA
   const dim3 grid((a.rows + per - 1) / per, a.Hkv, 2 * a.B);
-  if (a.D == 128) qread_kernel<TYPE, T, 128><<<grid, kReadThreads, 0, st>>>(a);
-  else qread_kernel<TYPE, T, 64><<<grid, kReadThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  if (a.D == 128) return launch_chained(true, qread_kernel<TYPE, T, 128>, grid, dim3(kReadThreads), 0, st, a);
+  return launch_chained(true, qread_kernel<TYPE, T, 64>, grid, dim3(kReadThreads), 0, st, a);
 }
 
 }  // namespace

@@ -643,4 +643,30 @@ def test_python_refusals():
                  lambda: api.QuantCache(c.shape, "e4m3", 64, c.K, c.V, c.K_scale, c.V_scale, c.bias, c.lengths.long())):
         with pytest.raises(S.SelKVError):
             call()
+    with pytest.raises(AttributeError):  # the tensors of a cache are not replaced
+        c.bias = None
     torch.cuda.synchronize()
+
+
+def test_calls_allocate_on_the_stream_they_run_on():
+    """Without a workspace and outputs given, on the default stream's handle, a side stream and its handle: the same
+    results, while other work allocates and frees on the current stream."""
+    c, g = filled("bf16", 2, 8, 2, 128, 300, "e4m3", 32, [280, 100], 51)
+    q = torch.randn((2, 8, 128), generator=g, device="cuda").bfloat16()
+    want, rows_want = api.decode_quant(c, q), api.quant_read(c, 3, 200)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (0, side, side.cuda_stream):
+        for _ in range(20):
+            out, back = api.decode_quant(c, q, stream=stream), api.quant_read(c, 3, 200, stream=stream)
+            junk = [torch.full((1 << k,), 7.0, device="cuda") for k in range(8, 20, 3)]
+            del junk
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(back[0], rows_want[0]) and torch.equal(back[1], rows_want[1])
+    full = api.alloc_compressed(c.shape)
+    full.K_c.normal_(generator=g), full.V_c.normal_(generator=g)
+    full.lengths.fill_(290)
+    torch.cuda.synchronize()
+    a, b = api.quantize(full, "int8", 64), api.quantize(full, "int8", 64, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(a.K, b.K) and torch.equal(a.V_scale, b.V_scale) and a.lengths.tolist() == [290, 290]
