@@ -167,6 +167,26 @@ def test_append_special_values(kind, dtype):
             model.check()
 
 
+@pytest.mark.parametrize("kind,dtype,B,H,d,block", [("int8", "bf16", 40, 32, 64, 32), ("e4m3", "fp32", 70, 8, 128, 128),
+                                                  ("e4m3", "bf16", 90, 16, 128, 16)])
+def test_append_of_many_tiles(kind, dtype, B, H, d, block):
+    """So many tiles that a CTA takes several of them: ragged prompts, then a chunk behind them; a NaN in one."""
+    g = gen(B)
+    cap, n0, n1 = 700, 500, 190
+    c = make(dtype, B, H, H, d, cap, kind, block)
+    model = Model(c)
+    ws = api.Workspace(S.selkv_qcache_workspace_size(c.shape))
+    for n in (n0, n1):
+        k, v = rows(g, B, H, n, d, dtype), rows(g, B, H, n, d, dtype)
+        counts = [(i * 97) % (n + 1) for i in range(B)]
+        counts[B // 2] = n
+        v[B // 2, H - 1, n - 1, 5] = math.nan
+        api.quant_append(c, k, v, None, torch.tensor(counts, dtype=torch.int32, device="cuda"), workspace=ws)
+        assert ws.errors() == S.SELKV_DEVERR_VALUE
+        model.append(k, v, counts)
+        model.check()
+
+
 def test_append_flags():
     """Rows that do not fit are not written, lengths and counts out of range are clamped; both are said."""
     g = gen(2)
