@@ -388,13 +388,13 @@ typedef struct selkv_qcache {
  * rows      row capacity of K_new, V_new and bias_new per (b, kv), at least 1.
  * K_new, V_new  [B][Hkv][rows][d] of the shape's dtype; bias_new [B][Hkv][rows] fp32 or NULL.
  * counts    [B] int32 device, 0 .. rows, or NULL: all `rows` rows.  (The lengths that
- *           selkv_compress wrote are the counts of its K_c, V_c and bias.)  Must not be the
- *           cache's own lengths.
+ *           selkv_compress wrote are the counts of its K_c, V_c and bias.)  Must not overlap
+ *           the cache's own lengths.
  * A sequence whose rows would pass m_cap takes none of them and sets SELKV_DEVERR_CAPACITY; a length
  * or count out of range is clamped and sets SELKV_DEVERR_LENGTH.
  * Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor (bias, bias_new and counts may be
  * NULL), bias_new without a bias, a bad shape, type or block; SELKV_ERR_UNSUPPORTED for d not
- * in {64, 128}; SELKV_ERR_WORKSPACE when workspace_bytes < selkv_qcache_workspace_size. */
+ * in {64, 128} and more than 2^30 rows; SELKV_ERR_WORKSPACE when workspace_bytes < selkv_qcache_workspace_size. */
 SELKV_API size_t selkv_qcache_workspace_size(const selkv_shape* shape);
 
 SELKV_API selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv_qcache* cache, int32_t rows,
@@ -423,7 +423,8 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite
  * number are the limit of very small weights (rows that all have it share the weight).  An append
  * that would pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
- * Workspaces: the two kinds are not interchangeable (a decode's is sized for its partials); each is
+ * Workspaces: the two kinds are not interchangeable (a decode's is sized for its partials; 0 for a shape that
+ * no cache has); each is
  * initialised once with selkv_workspace_init.
  * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */
 SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);

@@ -168,6 +168,12 @@ DecodeQPlan plan_decode_q(const selkv_shape& s) {
   return p;
 }
 
+// (The kernels count rows in 32 bits, up to a grid of tiles behind the last one.)
+constexpr int32_t kMaxQRows = 1 << 30;
+bool qcache_rows_ok(const selkv_shape& s) {
+  return s.m_cap >= 1 && s.m_cap <= kMaxQRows && (s.head_dim == 64 || s.head_dim == 128);
+}
+
 // SELKV_OK when `c` is a cache of shape `s`, and its kernel form in *q.
 selkv_status qcache_of(const selkv_shape& s, const selkv_qcache* c, QCache* q) {
   if (c == nullptr || (c->type != SELKV_Q_E4M3 && c->type != SELKV_Q_INT8)) return SELKV_ERR_INVALID_ARG;
@@ -177,7 +183,7 @@ selkv_status qcache_of(const selkv_shape& s, const selkv_qcache* c, QCache* q) {
   for (const void* t : tensors)
     if (t == nullptr || !aligned(t, 16)) return SELKV_ERR_INVALID_ARG;
   if (c->bias != nullptr && !aligned(c->bias, 16)) return SELKV_ERR_INVALID_ARG;
-  if (s.head_dim != 64 && s.head_dim != 128) return SELKV_ERR_UNSUPPORTED;
+  if (!qcache_rows_ok(s)) return SELKV_ERR_UNSUPPORTED;
   q->type = c->type;
   q->block_log2 = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
   q->nblk = (int)(((int64_t)s.m_cap + c->block - 1) / c->block);
@@ -583,7 +589,9 @@ selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv_qcache* c
   if (rows < 1 || K_new == nullptr || V_new == nullptr || !aligned(K_new, 16) || !aligned(V_new, 16))
     return SELKV_ERR_INVALID_ARG;
   if (bias_new != nullptr && (cache->bias == nullptr || !aligned(bias_new, 16))) return SELKV_ERR_INVALID_ARG;
-  if (counts != nullptr && (!aligned(counts, 4) || counts == cache->lengths)) return SELKV_ERR_INVALID_ARG;
+  if (counts != nullptr && (!aligned(counts, 4) || (counts < cache->lengths + s.batch && cache->lengths < counts + s.batch)))
+    return SELKV_ERR_INVALID_ARG;
+  if (rows > kMaxQRows) return SELKV_ERR_UNSUPPORTED;
   if (workspace == nullptr || !aligned(workspace, 256)) return SELKV_ERR_WORKSPACE;
   if (workspace_bytes < selkv_qcache_workspace_size(shape)) return SELKV_ERR_WORKSPACE;
   a.dtype = s.dtype;
@@ -630,7 +638,7 @@ selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cac
 }
 
 size_t selkv_decode_q_workspace_size(const selkv_shape* shape) {
-  if (!shape_ok(shape)) return 0;
+  if (!shape_ok(shape) || !qcache_rows_ok(*shape)) return 0;
   return plan_decode_q(*shape).total;
 }
 

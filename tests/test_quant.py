@@ -154,3 +154,24 @@ def test_python_refusals_on_the_host():
         api.alloc_quant(s, "int8", 24, device="cpu")
     with pytest.raises(S.SelKVError, match="CUDA"):  # a cache lives on a GPU
         api.alloc_quant(s, "int8", 64, device="cpu")
+
+
+def test_rows_out_of_range(lib):
+    """No rows, and more than are counted in 32 bits: a size of 0 and refusals."""
+    for m_cap in (0, 2 ** 30 + 1, 2 ** 31 - 1):
+        s = shape(batch=1, num_q_heads=4, num_kv_heads=1, m_cap=m_cap)
+        assert S.selkv_decode_q_workspace_size(s) == 0
+        want = S.SELKV_ERR_INVALID_ARG if m_cap == 0 else S.SELKV_ERR_UNSUPPORTED
+        assert append(s=s) == want and read(s=s) == want and dec(s=s) == want
+    assert S.selkv_decode_q_workspace_size(shape(head_dim=96)) == 0
+    assert S.selkv_decode_q_workspace_size(shape(batch=1, num_q_heads=4, num_kv_heads=1, m_cap=2 ** 30)) > 0
+    assert append(rows=2 ** 30 + 1) == S.SELKV_ERR_UNSUPPORTED
+
+
+def test_counts_overlap_the_lengths(lib):
+    """Counts that share some of their bytes with the cache's own lengths (two sequences)."""
+    for at in (-4, 0, 4):
+        assert append(s=shape(batch=2), c=cache(lengths=FAKE), counts=FAKE + at) == S.SELKV_ERR_INVALID_ARG
+    # (beside them they are taken: the next check refuses)
+    for at in (-8, 8):
+        assert append(s=shape(batch=2), c=cache(lengths=FAKE), counts=FAKE + at, ws=0) == S.SELKV_ERR_WORKSPACE
