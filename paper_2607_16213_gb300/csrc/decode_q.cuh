@@ -388,9 +388,8 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
       ve[h] = (float)((int)(__float_as_uint(cur.vs[h]) >> 23) - 127);
       vm[h] = __uint_as_float((__float_as_uint(cur.vs[h]) & 0x7fffffu) | 0x3f800000u);
     }
-    const float vmax = fmaxf(ve[0], ve[1]);
-    float corr[NT][2];
-    bool grew = false;
+    // The largest logit, and (tr, vr) that of the half of the tile whose largest weight times scale sets the units.
+    float tr[NT][2], vr[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -399,6 +398,33 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
         t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
+        tr[n][e] = t;
+        vr[n][e] = ve[0];
+      }
+    if (ve[0] != ve[1]) {  // (all lanes alike)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float th[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            th[h] = fmaxf(x[n][h][e], x[n][h][2 + e]);
+#pragma unroll
+            for (int m = 4; m < 32; m *= 2) th[h] = fmaxf(th[h], __shfl_xor_sync(0xffffffffu, th[h], m));
+          }
+          const bool first = (th[0] - th[1]) + (ve[0] - ve[1]) > 0.f;  // (no: neither half has a weight)
+          tr[n][e] = first ? th[0] : th[1];
+          vr[n][e] = first ? ve[0] : ve[1];
+        }
+    }
+    float corr[NT][2];
+    bool grew = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float t = tm[n][e];
         const float mn = fmaxf(mrow[n][e], t), mnr = mn == -INFINITY ? 0.f : mn;
         float sum = 0.f;
 #pragma unroll
@@ -414,10 +440,10 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) vo
         // O is in units of 2^(xref + kref - 10); the units grow only when a weight would pass 2^15.
         // (The logits are subtracted first: next to the lowest numbers ve would vanish.)
         corr[n][e] = 1.f;
-        if ((t - xref[n][e]) + vmax > kref[n][e] + 4.f) {  // (never with t = -inf)
-          corr[n][e] = ex2_approx((xref[n][e] - t) + (kref[n][e] - vmax));
-          xref[n][e] = t;
-          kref[n][e] = vmax;
+        if ((tr[n][e] - xref[n][e]) + vr[n][e] > kref[n][e] + 4.f) {  // (never with tr = -inf)
+          corr[n][e] = ex2_approx((xref[n][e] - tr[n][e]) + (kref[n][e] - vr[n][e]));
+          xref[n][e] = tr[n][e];
+          kref[n][e] = vr[n][e];
           grew = true;
         }
         const float d = mnr - xref[n][e] - kref[n][e] + 10.f;  // (+inf while no row has had a weight: the weights are 0)

@@ -642,6 +642,39 @@ def test_rows_without_weight_may_hold_anything():
     check_out(c, model, api.decode_quant(c, q), q)
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype,hq", [("bf16", 4), ("bf16", 24), ("fp32", 4), ("fp32", 20)])
+def test_decode_halves_of_a_tile_apart(kind, dtype, hq):
+    """Blocks of 16 rows, two to a tile: every other one holds values of 1e30 (or 1e12) that the bias gives no weight, or a
+    weight that still counts.  The others' digits stay: the units of the weights follow the half whose weight times scale
+    is the largest, so that the floor of `bound` is that of rows, not of tiles."""
+    B, hkv, d, cap, n = 6, 2, 64, 640, 615
+    c = make(dtype, B, hq, hkv, d, cap, kind, 16)
+    g = gen(77)
+    k, v = (torch.randn((B, hkv, n, d), generator=g, device="cuda") for _ in range(2))
+    bias = torch.zeros((B, hkv, n), device="cuda")
+    low = torch.finfo(torch.float32).min
+    for b, (odd, size, weight) in enumerate([(0, 1e30, -math.inf), (1, 1e30, -math.inf), (0, 1e30, low), (1, 1e30, low),
+                                             (1, 1e12, -25.0), (0, 1e-12, 20.0)]):
+        at = torch.arange(n, device="cuda") // 16 % 2 == odd
+        v[b, :, at] *= size
+        bias[b, :, at] = weight
+    v[5, :, 300:] = 0
+    k, v = k.to(TORCH[dtype]), v.to(TORCH[dtype])
+    api.quant_append(c, k, v, bias)
+    model = Model(c)
+    q = torch.randn((B, hq, d), generator=g, device="cuda").to(TORCH[dtype])
+    got, qs, G = np64(api.decode_quant(c, q)), np64(q), hq // hkv
+    for b in range(B):
+        for h in range(hkv):
+            kk, vv = model.head(b, h)
+            want, pv, mag, x, p = R.decode_head(qs[b, h * G:(h + 1) * G], kk, vv, model.bias[b, h, :n])
+            top = (p * model.vs[b, h][np.arange(n) // 16]).max(1)
+            lim = bound(dtype, want, pv, mag, x, n, n * R.QMAX[kind] * 2.0 ** -35 * top[:, None])
+            err = np.abs(got[b, h * G:(h + 1) * G] - want)
+            assert (err <= lim).all(), (b, h, float((err / lim).max()))
+
+
 def test_python_refusals():
     c, g = filled("bf16", 2, 8, 2, 128, 100, "e4m3", 64, [50, 3], 1)
     q = torch.zeros((2, 8, 128), dtype=torch.bfloat16, device="cuda")
