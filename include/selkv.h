@@ -421,7 +421,8 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * q, out        [B][Hq][d] of the shape's dtype; k_new, v_new [B][Hkv][d] or both NULL.
  * A row whose bias is -inf has no weight, whatever its codes, and a head whose rows all have none
  * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite
- * number are the limit of very small weights (rows that all have it share the weight).  An append
+ * number are the limit of very small weights (rows that all have it share the weight); weights below 2^-126
+ * of the largest count as none.  Without a cache's bias (NULL) none is read and none is written.  An append
  * that would pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
  * Workspaces: the two kinds are not interchangeable (a decode's is sized for its partials; 0 for a shape that
  * no cache has); each is

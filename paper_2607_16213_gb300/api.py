@@ -195,6 +195,14 @@ def _elsewhere(device: torch.device, stream) -> bool:
     return stream is not None or _current_device() != device.index
 
 
+def _space(workspace: Optional[Workspace], size, shape, device: torch.device, stream) -> Workspace:
+    if workspace is None:
+        return Workspace(size(shape), device, stream)
+    if workspace.buf.get_device() != device.index:
+        _bad("a workspace on %s is wanted, not on %s" % (device, workspace.buf.device))
+    return workspace
+
+
 @contextlib.contextmanager
 def _on(device: torch.device, stream):
     """The cache's device current, and allocations made on the stream that the call runs on."""
@@ -220,7 +228,7 @@ def quant_append(cache: QuantCache, K_new: torch.Tensor, V_new: torch.Tensor, bi
         _tensor(bias_new, "quant_append: bias_new", want[:3], torch.float32, dev)
     if counts is not None:
         _tensor(counts, "quant_append: counts", (s.batch,), torch.int32, dev)
-    ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+    ws = _space(workspace, B.selkv_qcache_workspace_size, s, dev, st)
     B.check(B.selkv_qcache_append(s, cache._bias, T, K_new, V_new, bias_new, counts, ws.buf, ws.nbytes, st),
             "selkv_qcache_append")
     return cache
@@ -256,7 +264,7 @@ def quant_read(cache: QuantCache, row0: int = 0, rows: Optional[int] = None, out
     K, V = out
     _tensor(K, "quant_read: K", want, cache._dtype, dev)
     _tensor(V, "quant_read: V", want, cache._dtype, dev)
-    ws = workspace or Workspace(B.selkv_qcache_workspace_size(s), dev, st)
+    ws = _space(workspace, B.selkv_qcache_workspace_size, s, dev, st)
     B.check(B.selkv_qcache_read(s, cache._bias, row0, rows, K, V, ws.buf, ws.nbytes, st), "selkv_qcache_read")
     return K, V
 
@@ -265,7 +273,8 @@ def decode_quant(cache: QuantCache, q: torch.Tensor, k_new: Optional[torch.Tenso
                  v_new: Optional[torch.Tensor] = None, use_bias: bool = True, out: Optional[torch.Tensor] = None,
                  workspace: Optional[Workspace] = None, stream=None) -> torch.Tensor:
     """selkv_decode_attn_q: one token [B][Hq][d] over an 8-bit cache (optionally appending k_new / v_new
-    [B][Hkv][d])."""
+    [B][Hkv][d]).  A row is not appended with use_bias off to a cache that has a bias: its bias would be left unset
+    (a QuantCache of the same tensors without the bias takes it)."""
     s, dev = cache.shape, cache.K.device
     if _elsewhere(dev, stream):
         with _on(dev, stream):
@@ -277,11 +286,13 @@ def decode_quant(cache: QuantCache, q: torch.Tensor, k_new: Optional[torch.Tenso
         new = (s.batch, s.num_kv_heads, s.head_dim)
         _tensor(k_new, "decode_quant: k_new", new, dt, dev)
         _tensor(v_new, "decode_quant: v_new", new, dt, dev)
+        if not use_bias and cache.bias is not None:
+            _bad("decode_quant: a row appended without the cache's bias")
     if out is None:
         out = torch.empty_like(q)
     else:
         _tensor(out, "decode_quant: out", want, dt, dev)
-    ws = workspace or Workspace(B.selkv_decode_q_workspace_size(s), dev, st)
+    ws = _space(workspace, B.selkv_decode_q_workspace_size, s, dev, st)
     B.check(B.selkv_decode_attn_q(s, cache._bias if use_bias else cache._plain, q, k_new, v_new, out, ws.buf, ws.nbytes, st),
             "selkv_decode_attn_q")
     return out

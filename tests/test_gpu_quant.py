@@ -675,6 +675,21 @@ def test_decode_halves_of_a_tile_apart(kind, dtype, hq):
             assert (err <= lim).all(), (b, h, float((err / lim).max()))
 
 
+def test_a_row_is_not_appended_without_the_bias():
+    """With use_bias off a new row would leave its bias unset: refused, unless the cache has none."""
+    c, g = filled("bf16", 1, 4, 2, 64, 100, "e4m3", 32, [60], 8)
+    q = torch.randn((1, 4, 64), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((1, 2, 64), generator=g, device="cuda").bfloat16() for _ in range(2))
+    with pytest.raises(S.SelKVError, match="bias"):
+        api.decode_quant(c, q, k, v, use_bias=False)
+    model = Model(c)
+    model.bias = None
+    plain = api.QuantCache(c.shape, "e4m3", 32, c.K, c.V, c.K_scale, c.V_scale, None, c.lengths)
+    check_out(plain, model, api.decode_quant(plain, q, k, v, use_bias=False), q, [True], k, v)
+    with pytest.raises(S.SelKVError, match="workspace"):
+        api.decode_quant(c, q, workspace=type("Host", (), {"buf": torch.zeros(1 << 16, dtype=torch.uint8), "nbytes": 1 << 16})())
+
+
 def test_python_refusals():
     c, g = filled("bf16", 2, 8, 2, 128, 100, "e4m3", 64, [50, 3], 1)
     q = torch.zeros((2, 8, 128), dtype=torch.bfloat16, device="cuda")
