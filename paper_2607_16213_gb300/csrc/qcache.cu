@@ -3,8 +3,8 @@
 // Append: a CTA takes 128 rows of the cache at a time, aligned to 128, of one KV head's K or V: whole blocks, so
 // no two CTAs share a scale.  A warp takes 8 or 16 of the rows and keeps them in registers between the
 // largest magnitude and the codes: an element is read once and a code written once.  Read: a thread takes 16
-// codes twice.  Both are bound by HBM: 131072 x 8 rows of bf16 and d 128 are written in 122 us (805 MB, 6.6
-// TB/s), eight ragged caches of 8192-16384 x 8 read in 90.5 us (557 MB, 6.2 TB/s).
+// codes at a time.  Both are bound by HBM: 131072 x 8 rows of bf16 and d 128 are written in 122 us (805 MB, 6.6
+// TB/s), eight ragged caches of 8192-16384 x 8 read in 87 us (557 MB, 6.4 TB/s).
 #include <algorithm>
 
 #include "quant.cuh"
@@ -224,7 +224,7 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-constexpr int kReadThreads = 128, kReadLoads = 2;
+constexpr int kReadThreads = 256;
 
 template <int TYPE, typename T, int D>
 __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
@@ -241,22 +241,11 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
   const uint8_t* codes = (isv ? a.c.V : a.c.K) + (bk * a.m_cap + a.row0) * D;
   const float* scales = (isv ? a.c.vs : a.c.ks) + bk * a.c.nblk;
   T* out = static_cast<T*>(isv ? a.v_out : a.k_out) + bk * a.rows * D;
-  const int i0 = blockIdx.x * (kReadThreads * kReadLoads) + threadIdx.x;  // 16 codes each
-  if (blockIdx.x * (kReadThreads * kReadLoads) / (D / 16) >= n) return;
-  uint4 w[kReadLoads];
-  float s[kReadLoads];
-#pragma unroll
-  for (int l = 0; l < kReadLoads; ++l) {
-    const int i = i0 + l * kReadThreads, row = i / (D / 16);
-    if (row >= n) continue;
-    w[l] = *reinterpret_cast<const uint4*>(codes + (size_t)i * 16);
-    s[l] = scales[(a.row0 + row) >> a.c.block_log2];
-  }
-#pragma unroll
-  for (int l = 0; l < kReadLoads; ++l) {
-    const int i = i0 + l * kReadThreads;
-    if (i / (D / 16) >= n) continue;
-    const uint32_t ws[4] = {w[l].x, w[l].y, w[l].z, w[l].w};
+  const size_t end = (size_t)n * (D / 16);  // 16 codes each
+  for (size_t i = blockIdx.x * kReadThreads + threadIdx.x; i < end; i += gridDim.x * kReadThreads) {
+    const uint4 w = *reinterpret_cast<const uint4*>(codes + i * 16);
+    const float s = scales[(a.row0 + (int)(i / (D / 16))) >> a.c.block_log2];
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float y[8], t[4];
@@ -264,9 +253,9 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
       for (int p = 0; p < 2; ++p) {
         C::unpack4(ws[j * 2 + p], t);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[p * 4 + e] = t[e] * s[l];
+        for (int e = 0; e < 4; ++e) y[p * 4 + e] = t[e] * s;
       }
-      store8(out + (size_t)i * 16 + j * 8, y);
+      store8(out + i * 16 + j * 8, y);
     }
   }
   // A decode over the rows may be the next kernel and load some before it waits for this one, once all of its CTAs
@@ -292,8 +281,11 @@ cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
 
 template <int TYPE, typename T>
 cudaError_t qread_t(const QReadArgs& a, cudaStream_t st) {
-  const int per = kReadThreads * kReadLoads * 16 / a.D;  // rows of a CTA
-  const dim3 grid((a.rows + per - 1) / per, a.Hkv, 2 * a.B);
+  // A CTA goes through its share of the rows, so that its fence is paid once: at most 64 CTAs for each SM in
+  // all (8 ragged caches of 8192-16384 x 8 rows: 86.9 us, with 16: 103, with a CTA for every 4 KB: 102).
+  const int per = kReadThreads * 16 / a.D;  // rows of a step
+  const long steps = (a.rows + per - 1) / per, units = 2L * a.B * a.Hkv;
+  const dim3 grid((unsigned)std::min(steps, (64L * kPlanSMs + units - 1) / units), a.Hkv, 2 * a.B);
   if (a.D == 128) return launch_chained(true, qread_kernel<TYPE, T, 128>, grid, dim3(kReadThreads), 0, st, a);
   return launch_chained(true, qread_kernel<TYPE, T, 64>, grid, dim3(kReadThreads), 0, st, a);
 }
