@@ -129,7 +129,7 @@ __device__ __forceinline__ float bias_log2(float b) {
 
 // NT: steps of eight heads.  fp32: queries and weights as two halves each.
 template <int TYPE, typename T, int D, int NT, int NW>
-__global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2 || sizeof(T) == 4)) void decode_q_kernel(
+__global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) void decode_q_kernel(
     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, QDecodeArgs a) {
   using C = QCfg<D, NT, NW>;
   constexpr int kWarps = C::kWarps, kThreads = C::kThreads;

@@ -163,7 +163,11 @@ struct QDecodePlan {
 QDecodePlan decode_q_plan(const selkv_shape& s);
 // CTA sizes: few (sequence, KV head) pairs get large CTAs, one on an SM (few splits to fold); many get
 // small ones.
-constexpr int ctas_of(int warps, bool wide) { return warps == 8 ? (wide ? 1 : 2) : wide ? 2 : 4; }  // CTAs on an SM
+// CTAs on an SM, as registers allow (wide: more than eight heads).
+constexpr int ctas_of(int warps, bool wide, bool fp32, int d) {
+  if (!wide && !fp32) return warps == 8 ? 2 : 4;
+  return warps == 8 ? 1 : d == 64 && !(wide && fp32) ? 3 : 2;
+}
 constexpr int kMaxSplits = kPlanSMs;
 // Floats of a (sequence, KV head)'s record of partials, where there are several clusters (Sg).
 __host__ __device__ constexpr size_t decode_q_record_floats(int G, int Sc, int Sg, int D) {
