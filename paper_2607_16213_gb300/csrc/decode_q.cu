@@ -1,8 +1,6 @@
 // How a decode over an 8-bit cache is split (the kernels are in decode_q.cuh, a file for each type).
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
-#include <cstdio>
 
 #include "quant.cuh"
 
@@ -69,7 +67,6 @@ QDecodePlan plan_of(const selkv_shape& s) {
 
 // (The search takes some microseconds; a decode comes back with the same shape call after call.)
 QDecodePlan decode_q_plan(const selkv_shape& s) {
-  if (const char* e = getenv("SELKV_PLAN")) { QDecodePlan b{}; if (sscanf(e, "%d,%d,%d", &b.warps, &b.splits, &b.cluster) == 3) return b; }
   static thread_local selkv_shape of{};
   static thread_local QDecodePlan plan{};
   if (plan.warps == 0 || of.dtype != s.dtype || of.batch != s.batch || of.num_q_heads != s.num_q_heads ||
