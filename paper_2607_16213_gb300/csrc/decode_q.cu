@@ -21,7 +21,7 @@ namespace selkv {
 //   256 x 2      one split: 4.1; a cluster of 2: 4.9
 // The constants below were fitted to the times of all plans (caches larger than L2, a row appended) for 744 batches:
 // 1 to 1024 heads, 90 to 130000 rows, 1 to 16 query heads, d 64 and 128, both types, full and ragged.  The plan that
-// they choose takes 0.8 percent more than the best one on average and 15 percent at most; of 80 other batches 1.6 and 12.
+// they choose takes 0.9 percent more than the best one on average and 15 percent at most; of 80 other batches 1.7 and 12.
 namespace {
 double plan_us(const selkv_shape& s, int warps, int S, int cluster) {
   const bool wide = s.num_q_heads / s.num_kv_heads > 8, fp32 = s.dtype == SELKV_FP32;
@@ -37,7 +37,9 @@ double plan_us(const selkv_shape& s, int warps, int S, int cluster) {
   const double cta_rows = std::ceil(std::ceil(rows / S) / 64) * 64;
   const double work = waves * cta_rows / (warps * 32) * kRound[warps == 8][(int)share - 1] *
                       (s.head_dim == 64 ? 0.89 : 1) * (fp32 ? 0.89 : 1) * (wide ? 1.1 : 1);
-  const double hbm = 0.9 * n * rows * s.head_dim * 2 / 6.4e6 * (1 + 0.29 * idle);
+  // (what an SM has in flight, in 64 KB: more than that queues up; 131072 x 8 rows: 44.7 us with 64 KB, 45.6 with 128)
+  const double flight = share * warps * s.head_dim / 1024;
+  const double hbm = 0.9 * n * rows * s.head_dim * 2 / 6.4e6 * (1 + 0.29 * idle) * (1 + 0.04 * std::max(0.0, flight - 1));
   const double both = std::cbrt(work * work * work + hbm * hbm * hbm);  // (the larger of the two, rounded off)
   return both + 2.6 * (waves - 1) + 0.26 * (share - 1) +
          (cluster == 1 ? 0 : (cluster == 2 ? 1.0 : cluster == 4 ? 1.1 : 1.5) + 0.11 * (partial - 1)) +

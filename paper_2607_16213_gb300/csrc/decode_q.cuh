@@ -7,7 +7,7 @@
 // a stream of its own: it takes every kWarps-th tile of 32 rows, which its lane 0 brings into the warp's own
 // shared memory with two 2D TMA loads (K and V; the next K as soon as this one is multiplied, the next V
 // likewise), so no warp waits for another in the loop.  64 KB in flight on an SM is as much as helps:
-// with 128 KB one token over 131072 x 8 rows takes 45.5 us instead of 44.6, with 192 KB 49.8, as whatever is
+// with 128 KB one token over 131072 x 8 rows takes 45.6 us instead of 44.7, with 192 KB 49.8, as whatever is
 // asked for queues behind it.
 //
 // Per tile S^T = K Q^T and O^T += V^T P^T run on the tensor cores (mma.sync m16n8k16): the rows and the
@@ -23,7 +23,7 @@
 // weights down to 2^-24 of the largest keep 11 bits (fp32 caches: 22, as two halves).
 //
 // A key row costs 2 d + 4 bytes of HBM and 4 G d flops.  What bounds it: HBM from some tens of MB on
-// (131072 x 8 rows of d 128, 269 MB: 44.6 us, 6.0 TB/s of 6.8 measured for a copy); below that the way in
+// (131072 x 8 rows of d 128, 269 MB: 44.7 us, 6.0 TB/s of 6.8 measured for a copy); below that the way in
 // (length, queries and the first tiles: 3 us) and out (fold of warps and splits: 2 to 4 us); for d 64
 // the work of a tile, which is that of d 128 but for half of the products.
 #pragma once
