@@ -424,9 +424,9 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * number are the limit of very small weights (rows that all have it share the weight); weights below 2^-126
  * of the largest count as none.  Without a cache's bias (NULL) none is read and none is written.  An append
  * that would pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
- * Workspaces: the two kinds are not interchangeable (a decode's is sized for its partials; 0 for a shape that
- * no cache has); each is
- * initialised once with selkv_workspace_init.
+ * Workspaces: initialised once with selkv_workspace_init, one serves selkv_qcache_append, selkv_qcache_read and this call over any
+ * caches, one after another, that it is large enough for (a decode's size counts its partials and is enough
+ * for the other two; 0 for a shape that no cache has).
  * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */
 SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);
 

@@ -141,9 +141,10 @@ DecodePlan plan_decode(const selkv_shape& s) {
   return p;
 }
 
-// Decode over 8-bit caches.
+// Decode over 8-bit caches.  The counters lie at the same place for every shape (and cnt_seq where an append has it): they
+// are zero after each call, and no call's partials reach them, so that a workspace may go from one cache to another.
 struct DecodeQPlan {
-  size_t cnt_head, cnt_seq, partial, total;
+  size_t cnt_seq, cnt_head, partial, total;
   int splits, warps, cluster;
 };
 
@@ -161,8 +162,8 @@ DecodeQPlan plan_decode_q(const selkv_shape& s) {
   p.warps = q.warps;
   p.cluster = q.cluster;
   const int clusters = q.splits / q.cluster;
-  p.cnt_head = take(bk * q.cluster * 4);
-  p.cnt_seq = take((size_t)s.batch * 4);
+  p.cnt_seq = take((size_t)SELKV_MAX_BATCH * 4);
+  p.cnt_head = take((size_t)kMaxQSplitCtas * 4);  // (used where clusters > 1: B Hkv cluster of them, fewer than CTAs)
   p.partial = take(clusters > 1 ? bk * decode_q_record_floats(s.num_q_heads / s.num_kv_heads, q.cluster, clusters, s.head_dim) * 4 : 0);
   p.total = off;
   return p;

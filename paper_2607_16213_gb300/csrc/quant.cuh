@@ -164,11 +164,14 @@ QDecodePlan decode_q_plan(const selkv_shape& s);
 // CTA sizes: few (sequence, KV head) pairs get large CTAs, one on an SM (few splits to fold); many get
 // small ones.
 // CTAs on an SM, as registers allow (wide: more than eight heads).
+constexpr int kMaxQCtas = 4;
 constexpr int ctas_of(int warps, bool wide, bool fp32, int d) {
-  if (!wide && !fp32) return warps == 8 ? 2 : 4;
+  if (!wide && !fp32) return warps == 8 ? 2 : kMaxQCtas;
   return warps == 8 ? 1 : d == 64 && !(wide && fp32) ? 3 : 2;
 }
 constexpr int kMaxSplits = kPlanSMs;
+// CTAs of a decode whose (sequence, KV head) pairs are split, all together: two waves (plan_of).
+constexpr int kMaxQSplitCtas = 2 * kPlanSMs * kMaxQCtas;
 // Floats of a (sequence, KV head)'s record of partials, where there are several clusters (Sg).
 __host__ __device__ constexpr size_t decode_q_record_floats(int G, int Sc, int Sg, int D) {
   return (size_t)G * Sg * D + (((size_t)Sc * G * Sg * 2 + 3) & ~(size_t)3);
