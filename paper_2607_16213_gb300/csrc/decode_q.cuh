@@ -449,9 +449,16 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
         const float d = mnr - xref[n][e] - kref[n][e] + 10.f;  // (+inf while no row has had a weight: the weights are 0)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float f = vm[h] * ex2_approx(fminf(d + ve[h], 120.f));
+          const float up = d + ve[h], f = vm[h] * ex2_approx(fminf(up, 120.f));
 #pragma unroll
           for (int q = 0; q < 2; ++q) x[n][h][q * 2 + e] *= f;
+          // Weights are 2^-126 and more and their products with f below 2^15, so up is below 142 where there are any: the
+          // part beyond an exponent's range is a second factor.
+          if (up > 120.f) {
+            const float f2 = ex2_approx(fminf(up, 142.f) - 120.f);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) x[n][h][q * 2 + e] *= f2;
+          }
         }
       }
     if (__any_sync(0xffffffffu, grew)) {
@@ -567,11 +574,13 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][hd]);
       const bool none = mrow[n][e] == -INFINITY;  // this warp has no row with a weight
-      const float f = none ? 0.f : ex2_approx((xref[n][e] - M) + (kref[n][e] - 10.f));
+      // (two factors where one would be below 2^-126: a weight may be that small, and its row's scale too)
+      const float down = (xref[n][e] - M) + (kref[n][e] - 10.f);
+      const float f = none ? 0.f : ex2_approx(fmaxf(down, -100.f)), f2 = down < -100.f ? ex2_approx(down + 100.f) : 1.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         *reinterpret_cast<float2*>(wo + (warp * GU + hd) * C::kFoldLd + c * 16 + 2 * g) =
-            make_float2(o[n][c][e] * f, o[n][c][2 + e] * f);
+            make_float2(o[n][c][e] * f * f2, o[n][c][2 + e] * f * f2);
       if (g == 0) {
         wl[warp][hd] = none ? lrow[n][e] : lrow[n][e] * ex2_approx(mrow[n][e] - M);
         if (warp == 0) s_M[hd] = M;

@@ -1,13 +1,15 @@
 """Caches held in 8 bits at their edges, against the plain form in 64 bits: workspaces that go from one cache to
-another."""
+another, weights far below the largest."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2607_16213_gb300 as S
 from paper_2607_16213_gb300 import api
-from test_gpu_quant import Model, filled, gen, rows
+import quant_ref as R
+from test_gpu_quant import Model, TORCH, filled, gen, make, np64, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +69,50 @@ def test_a_decode_workspace_serves_append_and_read():
         assert torch.equal(K[0, 1].cpu(), torch.from_numpy(model.head(0, 1)[0][16:116]).bfloat16())
     model.check()
     assert ws.errors() == 0
+
+
+# ---- weights far below the largest --------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("gap", [90, 109, 112, 115, 118, 121, 124])
+@pytest.mark.parametrize("B,hkv,n", [(40, 8, 700), (5, 2, 5000)])
+def test_decode_weights_far_below_the_largest(kind, dtype, zeros, gap, B, hkv, n):
+    """Sixteen rows of values around 1 (or 0) with the largest logit, sixteen of values around 2^122 (or 2^10) with one `gap`
+    (in base 2) below: their share, weights above 2^-126 of the largest times huge values, is (all of) the output.
+    In the other half of a tile, in another tile of a warp, of a CTA or (few, long caches) of the batch, before and behind.
+
+    What it may be off, with u = 2^-24: the bias in base 2 is rounded twice (the constant, the product) and the difference of
+    two logits once, numbers below 128, so 3 x 64 u ln 2 = 133 u of a weight, and the exponential 4 u; both again for the
+    normaliser.  The units of the output and their fold: up to seven roundings of exponents below 256, 128 u ln 2 each, and
+    three exponentials: 633 u.  The weight in fp16 (2^-11; fp32 2^-21), sums of 32 products of positive numbers cut off, 64 u, folds
+    200 u, and the output's own rounding.  Codes of rows that count are three quarters of the largest and more."""
+    hq, d, block = hkv, 64, 16
+    at = {0: (0, 16), 1: (16, 0), 2: (0, 256), 3: (256, 0), 4: (640, 32)}  # first row of the large logits, of the others
+    c = make(dtype, B, hq, hkv, d, n + 20, kind, block)
+    g = gen(gap)
+    small, huge = (0.0, 2.0 ** 10) if zeros else (1.0, 2.0 ** 122)
+    V = torch.zeros((B, hkv, n, d), device="cuda")
+    bias = torch.full((B, hkv, n), -math.inf, device="cuda")
+    for b in range(B):
+        top, far = at[b % len(at)]
+        V[b, :, top:top + 16] = small * (0.75 + torch.rand((hkv, 16, d), generator=g, device="cuda") / 4)
+        V[b, :, far:far + 16] = huge * (0.75 + torch.rand((hkv, 16, d), generator=g, device="cuda") / 4)
+        bias[b, :, top:top + 16] = 0.0
+        bias[b, :, far:far + 16] = -gap * math.log(2)
+    K = torch.zeros_like(V)
+    api.quant_append(c, K.to(TORCH[dtype]), V.to(TORCH[dtype]), bias)
+    model = Model(c)
+    q = torch.randn((B, hq, d), generator=g, device="cuda").to(TORCH[dtype])
+    ws = api.Workspace(S.selkv_decode_q_workspace_size(c.shape))
+    got = np64(api.decode_quant(c, q, workspace=ws))
+    assert ws.errors() == 0
+    u = 2.0 ** -24
+    lim = (2 * 137 + 633 + 264) * u + (2.0 ** -11 + 2.0 ** -8 if dtype == "bf16" else 2.0 ** -21 + u)
+    for b in range(B):
+        for h in range(hkv):
+            kk, vv = model.head(b, h)
+            live = np.isfinite(model.bias[b, h, :n])
+            want = R.decode_head(np64(q)[b, h:h + 1], kk[live], vv[live], model.bias[b, h, :n][live])[0][0]
+            err = np.abs(got[b, h] - want) / want
+            assert err.max() <= lim, (b, h, float(err.max()), lim, got[b, h, :3], want[:3])
