@@ -422,8 +422,9 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * A row whose bias is -inf has no weight, whatever its codes, and a head whose rows all have none
  * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite
  * number are the limit of very small weights (rows that all have it share the weight); weights below 2^-126
- * of the largest count as none.  Without a cache's bias (NULL) none is read and none is written.  An append
- * that would pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
+ * of the largest count as none; a row whose bias is NaN makes its heads' outputs NaN.  Without a cache's
+ * bias (NULL) none is read and none is written.  An append that would pass m_cap is skipped and sets
+ * SELKV_DEVERR_CAPACITY (the output has no new row then).
  * Workspaces: initialised once with selkv_workspace_init, one serves selkv_qcache_append, selkv_qcache_read and this call over any
  * caches, one after another, that it is large enough for (a decode's size counts its partials and is enough
  * for the other two; 0 for a shape that no cache has).

@@ -122,9 +122,11 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packe
   return pack_f16(lo - t.x, hi - t.y);
 }
 
-// Bias in base 2.  The lowest finite numbers stay finite: rows that all have them share the weight.
+// Bias in base 2.  The lowest finite numbers stay finite: rows that all have them share the weight.  A NaN stays one (a
+// maximum would drop it).
 __device__ __forceinline__ float bias_log2(float b) {
-  return b == -INFINITY ? b : fmaxf(b * kLog2e, -3.402823466e38f);
+  const float x = b * kLog2e;
+  return x == -INFINITY && b != x ? -3.402823466e38f : x;
 }
 
 // NT: steps of eight heads.  fp32: queries and weights as two halves each.

@@ -1,5 +1,5 @@
 """Caches held in 8 bits at their edges, against the plain form in 64 bits: workspaces that go from one cache to
-another, weights far below the largest."""
+another, weights far below the largest, a NaN among the compensation."""
 import math
 
 import numpy as np
@@ -116,3 +116,27 @@ def test_decode_weights_far_below_the_largest(kind, dtype, zeros, gap, B, hkv, n
             want = R.decode_head(np64(q)[b, h:h + 1], kk[live], vv[live], model.bias[b, h, :n][live])[0][0]
             err = np.abs(got[b, h] - want) / want
             assert err.max() <= lim, (b, h, float(err.max()), lim, got[b, h, :3], want[:3])
+
+
+# ---- compensation that is no number ---------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype,hq", [("bf16", 4), ("bf16", 24), ("fp32", 4), ("fp32", 20)])
+@pytest.mark.parametrize("cap", [300, 9000])
+def test_decode_nan_bias(kind, dtype, hq, cap):
+    """A NaN in the bias of a row makes the outputs of its KV head's query heads NaN, as the formula does, and no other; also beside
+    rows without weight, and where it is the only row that is not masked."""
+    B, hkv, d = 4, 2, 64
+    lens = [cap - 20, cap - 60, 31, 1]
+    c, g = filled(dtype, B, hq, hkv, d, cap, kind, 32, lens, cap)
+    c.bias[0, 1, 100] = math.nan
+    c.bias[1, 0, :] = -math.inf
+    c.bias[1, 0, 200] = math.nan
+    c.bias[2, 1, :31] = torch.finfo(torch.float32).min
+    c.bias[2, 1, 30] = math.nan
+    c.bias[3, 0, 0] = math.nan
+    c.bias[3, 1, 1:] = math.nan  # behind the rows of the cache: not read
+    q = torch.randn((B, hq, d), generator=g, device="cuda").to(TORCH[dtype])
+    out = api.decode_quant(c, q).view(B, hkv, hq // hkv, d)
+    want = torch.zeros((B, hkv), dtype=torch.bool, device="cuda")
+    want[0, 1] = want[1, 0] = want[2, 1] = want[3, 0] = True
+    assert torch.equal(out.isnan().all(-1).all(-1), want) and torch.equal(out.isnan().any(-1).any(-1), want)
