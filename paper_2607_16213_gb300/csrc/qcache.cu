@@ -155,7 +155,7 @@ __global__ __launch_bounds__(ACfg<T, D>::kThreads, ACfg<T, D>::kCtas) void qappe
     const int blk = row0 >> a.c.block_log2, bfirst = blk << a.c.block_log2;
     const bool live = bfirst < L + n && bfirst + (1 << a.c.block_log2) > L;  // the block takes new rows
     const bool holds = live && L > bfirst;
-    const float s0 = holds ? fmaxf(scales[blk], kMinScale) : 0.f;  // read by every warp before one writes it
+    const float s0 = holds ? held_scale(scales[blk]) : 0.f;  // read by every warp before one writes it
     __syncthreads();
     if (!isv && a.c.bias != nullptr) {
       const int row = row0 + lane;

@@ -103,10 +103,12 @@ struct Code<SELKV_Q_INT8> {
   }
 };
 
-// Scale of a block with rows in it, for new rows of largest magnitude a.
+// Scale of a block with rows in it: any normal number, as the caller may have set it.  (Anything smaller or a NaN, which no
+// block with rows has, counts as the smallest fresh one.)
+__device__ __forceinline__ float held_scale(float s) { return s >= 1.1754943508222875e-38f ? s : kMinScale; }
+// The same for new rows of largest magnitude a.
 template <int TYPE>
 __device__ __forceinline__ float grown_scale(float old, float a) {
-  old = fmaxf(old, kMinScale);
   const float most = old * Code<TYPE>::kMax;
   if (!(a > most)) return old;
   int k = (int)(__float_as_uint(a) >> 23) - (int)(__float_as_uint(most) >> 23);
@@ -205,7 +207,7 @@ __device__ __forceinline__ void append_row(const T* x, uint8_t* codes, float* sc
   if (odd) raise_flag(flags, SELKV_DEVERR_VALUE);
   const int blk = L >> block_log2, first = blk << block_log2;
   const bool holds = L > first;
-  const float s0 = holds ? fmaxf(scales[blk], kMinScale) : 0.f;
+  const float s0 = holds ? held_scale(scales[blk]) : 0.f;
   const float s = holds ? grown_scale<TYPE>(s0, a) : C::fresh_scale(a);
   if (holds && s != s0) {
     const float f = s0 / s;  // 2^-k

@@ -1,5 +1,6 @@
 """Caches held in 8 bits at their edges, against the plain form in 64 bits: workspaces that go from one cache to
-another, weights far below the largest, a NaN among the compensation."""
+another, weights far below the largest, a NaN among the compensation, scales of the caller's own
+below the smallest fresh one."""
 import math
 
 import numpy as np
@@ -9,7 +10,7 @@ import torch
 import paper_2607_16213_gb300 as S
 from paper_2607_16213_gb300 import api
 import quant_ref as R
-from test_gpu_quant import Model, TORCH, filled, gen, make, np64, rows
+from test_gpu_quant import Model, TORCH, filled, gen, make, np64, rows, u8
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +141,43 @@ def test_decode_nan_bias(kind, dtype, hq, cap):
     want = torch.zeros((B, hkv), dtype=torch.bool, device="cuda")
     want[0, 1] = want[1, 0] = want[2, 1] = want[3, 0] = True
     assert torch.equal(out.isnan().all(-1).all(-1), want) and torch.equal(out.isnan().any(-1).any(-1), want)
+
+
+# ---- scales of the caller's own -------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("by", ["append", "decode"])
+@pytest.mark.parametrize("e0", [-126, -110, -101, -100, 20])
+def test_rows_behind_a_callers_scale(kind, dtype, by, e0):
+    """A block with rows and a scale that the caller set, any normal number: the scale is kept or grows by the smallest power of
+    two that covers the new row, and the old codes are rounded to it."""
+    B, H, d, block, L = 5, 2, 64, 32, 10
+    c = make(dtype, B, H, H, d, 64, kind, block, junk=False)
+    s0 = 2.0 ** e0
+    g = gen(e0 + 200)
+    code = torch.randint(-100, 101, (B, H, L, d), generator=g, device="cuda")
+    for t, s in ((c.K, c.K_scale), (c.V, c.V_scale)):
+        t[:, :, :L] = code.to(torch.int8) if kind == "int8" else code.float().to(torch.float8_e4m3fn)
+        s[:, :, 0] = s0
+    c.lengths.fill_(L)
+    # largest magnitudes of the new rows, in units of the scale: within its codes, and 1, 2, 5 and 30 doublings past them
+    most = R.QMAX[kind] * torch.tensor([0.5, 1.5, 3.0, 30.0, 2.0 ** 29 * 1.1], device="cuda")
+    x = (torch.rand((B, H, d), generator=g, device="cuda") - 0.5) * most[:, None, None]
+    x[:, :, 7] = most[:, None]
+    x = (x.double() * s0).to(TORCH[dtype])
+    old = [R.values(u8(t), kind)[:, :, :L] for t in (c.K, c.V)]
+    if by == "append":
+        api.quant_append(c, x[:, :, None].contiguous(), (-x)[:, :, None].contiguous())
+    else:
+        api.decode_quant(c, torch.zeros((B, H, d), dtype=TORCH[dtype], device="cuda"), x, -x)
+    assert c.lengths.tolist() == [L + 1] * B
+    for t, s, was, new in ((c.K, c.K_scale, old[0], np64(x)), (c.V, c.V_scale, old[1], -np64(x))):
+        got, scale = R.values(u8(t), kind), np64(s)
+        for b in range(B):
+            for h in range(H):
+                want = s0
+                while want * R.QMAX[kind] < np.abs(new[b, h]).max():
+                    want *= 2
+                assert scale[b, h, 0] == want
+                np.testing.assert_array_equal(got[b, h, :L], R.round_code(was[b, h] * (s0 / want), kind))
+                np.testing.assert_array_equal(got[b, h, L], R.round_code(new[b, h] / want, kind))
