@@ -303,7 +303,8 @@ SELKV_API selkv_status selkv_layer_average_bias(const selkv_shape* shape, const 
  * enqueued just before it on the same stream is still running.  That kernel must therefore
  * not write those rows of K_c and V_c (it may write q, k_new, v_new, the bias, lengths, and
  * row lengths[b] - 1 onwards).  The library's own calls never do: a decode appends only at
- * lengths[b], and a compression writes K_c and V_c before its last kernel.  A caller kernel
+ * lengths[b], and a compression and a selkv_qcache_read write their rows before their last
+ * kernel.  A caller kernel
  * that rewrites cached rows must be separated from the decode by another stream operation
  * (any other kernel, a copy or an event).  Everything the result is computed from is read
  * after the previous kernel has completed: rows loaded early are used only where the slice
@@ -405,8 +406,8 @@ SELKV_API selkv_status selkv_qcache_append(const selkv_shape* shape, const selkv
 /* Rows back out of the cache: rows row0 .. row0 + rows - 1 of each (b, kv) that lie below lengths[b], as
  * code * scale rounded once to the shape's dtype, into K_out and V_out [B][Hkv][rows][d].  Rows at
  * or behind lengths[b] of the outputs are left as they were.  0 <= row0, 1 <= rows,
- * row0 + rows <= m_cap.  The outputs may be K_c and V_c of a selkv_decode_attn that follows at once (the
- * one exception to "Overlap with the previous kernel").  Errors as above. */
+ * row0 + rows <= m_cap.  The outputs may be K_c and V_c of a selkv_decode_attn that follows at once (see
+ * "Overlap with the previous kernel": the call's last kernel writes none of them).  Errors as above. */
 SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cache, int32_t row0,
                                          int32_t rows, void* K_out, void* V_out, void* workspace,
                                          size_t workspace_bytes, selkv_stream_t stream);

@@ -634,7 +634,7 @@ selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_qcache* cac
   a.v_out = V_out;
   a.flags = at<uint32_t>(workspace, 0);
   const cudaError_t e = launch_qread(a, reinterpret_cast<cudaStream_t>(stream));
-  g_launches += 1;
+  g_launches += s.dtype == SELKV_BF16 ? 2 : 1;
   return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
 }
 

@@ -4,7 +4,7 @@
 // no two CTAs share a scale.  A warp takes 8 or 16 of the rows and keeps them in registers between the
 // largest magnitude and the codes: an element is read once and a code written once.  Read: a thread takes 16
 // codes at a time.  Both are bound by HBM: 131072 x 8 rows of bf16 and d 128 are written in 122 us (805 MB, 6.6
-// TB/s), eight ragged caches of 8192-16384 x 8 read in 87 us (557 MB, 6.4 TB/s).
+// TB/s), eight ragged caches of 8192-16384 x 8 read in 84 us (557 MB, 6.6 TB/s).
 #include <algorithm>
 
 #include "quant.cuh"
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
   using C = Code<TYPE>;
   const int h = blockIdx.y, b = blockIdx.z >> 1, isv = blockIdx.z & 1;
   const size_t bk = (size_t)b * a.Hkv + h;
-  pdl_wait();  // (the next kernel comes up when this one's CTAs have ended: it may load the rows written here)
+  chain_begin();
   int L = a.c.lengths[b];
   if (L < 0 || L > a.m_cap) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && h == 0 && isv == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
@@ -258,11 +258,11 @@ __global__ __launch_bounds__(kReadThreads) void qread_kernel(QReadArgs a) {
       store8(out + i * 16 + j * 8, y);
     }
   }
-  // A decode over the rows may be the next kernel and load some before it waits for this one, once all of its CTAs
-  // have ended: their rows are in place by then.
-  __syncthreads();
-  if (threadIdx.x == 0) __threadfence();
 }
+
+// The last kernel of a read into bf16 rows: it ends when they are in place.  A decode over them that follows loads rows
+// before it waits for the kernel in front of it, so that must not be the one that writes them.
+__global__ void qread_end_kernel() { pdl_wait(); }
 
 template <int TYPE, typename T>
 cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
@@ -281,13 +281,15 @@ cudaError_t qappend_t(const QAppendArgs& a, cudaStream_t st) {
 
 template <int TYPE, typename T>
 cudaError_t qread_t(const QReadArgs& a, cudaStream_t st) {
-  // A CTA goes through its share of the rows, so that its fence is paid once: at most 64 CTAs for each SM in
-  // all (8 ragged caches of 8192-16384 x 8 rows: 86.9 us, with 16: 103, with a CTA for every 4 KB: 102).
+  // A CTA goes through its share of the rows: at most 128 CTAs for each SM in all (8 ragged caches of 8192-16384 x 8
+  // rows: 84.1 us, with 64: 86.5, with 32: 95.0, with a CTA for every 4 KB: 88.5).
   const int per = kReadThreads * 16 / a.D;  // rows of a step
   const long steps = (a.rows + per - 1) / per, units = 2L * a.B * a.Hkv;
-  const dim3 grid((unsigned)std::min(steps, (64L * kPlanSMs + units - 1) / units), a.Hkv, 2 * a.B);
-  if (a.D == 128) return launch_chained(true, qread_kernel<TYPE, T, 128>, grid, dim3(kReadThreads), 0, st, a);
-  return launch_chained(true, qread_kernel<TYPE, T, 64>, grid, dim3(kReadThreads), 0, st, a);
+  const dim3 grid((unsigned)std::min(steps, (128L * kPlanSMs + units - 1) / units), a.Hkv, 2 * a.B);
+  const cudaError_t e = a.D == 128 ? launch_chained(true, qread_kernel<TYPE, T, 128>, grid, dim3(kReadThreads), 0, st, a)
+                                   : launch_chained(true, qread_kernel<TYPE, T, 64>, grid, dim3(kReadThreads), 0, st, a);
+  if (sizeof(T) == 4 || e != cudaSuccess) return e;
+  return launch_chained(true, qread_end_kernel, dim3(1), dim3(32), 0, st);
 }
 
 }  // namespace

@@ -181,3 +181,50 @@ def test_rows_behind_a_callers_scale(kind, dtype, by, e0):
                 assert scale[b, h, 0] == want
                 np.testing.assert_array_equal(got[b, h, :L], R.round_code(was[b, h] * (s0 / want), kind))
                 np.testing.assert_array_equal(got[b, h, L], R.round_code(new[b, h] / want, kind))
+
+
+# ---- rows read back, then decoded over ------------------------------------------------------------------
+@pytest.mark.parametrize("graph", [False, True])
+def test_the_kernel_in_front_of_a_decode_writes_no_rows(graph):
+    """A bf16 decode loads rows before it waits for the kernel in front of it: a read's rows are written by an earlier one of its two.
+    Reads of several caches into the same rows, a decode behind each, on a stream of their own and captured."""
+    B, hq, hkv, d, cap = 2, 16, 4, 128, 6000
+    shape = api.make_shape("bf16", B, hq, hkv, d, 32, cap, cap)
+    g = gen(61)
+    q = torch.randn((B, hq, d), generator=g, device="cuda").bfloat16()
+    caches = [filled("bf16", B, hq, hkv, d, cap, "int8", 64, [cap - 3 * i, cap - 500], i)[0] for i in range(3)]
+    full = api.alloc_compressed(shape)
+    full.lengths.fill_(cap - 501)
+    ws, wr = api.Workspace(S.selkv_decode_workspace_size(shape)), api.Workspace(S.selkv_qcache_workspace_size(shape))
+    outs = torch.empty((12, B, hq, d), dtype=torch.bfloat16, device="cuda")
+
+    def one(i, out, wait=False):
+        before = S.selkv_kernel_launches()
+        api.quant_read(caches[i % 3], out=(full.K_c, full.V_c), workspace=wr)
+        assert S.selkv_kernel_launches() == before + 2
+        if wait:
+            torch.cuda.synchronize()
+        api.decode(full, q, use_bias=False, out=out, workspace=ws, stream=torch.cuda.current_stream().cuda_stream)
+
+    want = torch.empty_like(outs[:3])
+    for i in range(3):
+        one(i, want[i], wait=True)
+    torch.cuda.synchronize()
+    assert not torch.equal(want[0], want[1])
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        if graph:
+            recorded = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(recorded, stream=stream):
+                for i in range(12):
+                    one(i, outs[i])
+            for _ in range(3):
+                outs.fill_(math.nan)
+                recorded.replay()
+        else:
+            for i in range(12):
+                one(i, outs[i])
+    torch.cuda.synchronize()
+    for i in range(12):
+        assert torch.equal(outs[i], want[i % 3]), i
+    assert ws.errors() == 0 and wr.errors() == 0
