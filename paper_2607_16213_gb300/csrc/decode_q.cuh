@@ -122,11 +122,11 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packe
   return pack_f16(lo - t.x, hi - t.y);
 }
 
-// Bias in base 2.  The lowest finite numbers stay finite: rows that all have them share the weight.  A NaN stays one (a
-// maximum would drop it).
+// Bias in base 2.  The lowest finite numbers stay finite: rows that all have them share the weight.  A NaN stays one.
 __device__ __forceinline__ float bias_log2(float b) {
-  const float x = b * kLog2e;
-  return x == -INFINITY && b != x ? -3.402823466e38f : x;
+  float x;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(b * kLog2e), "f"(-3.402823466e38f));
+  return b == -INFINITY ? b : x;
 }
 
 // NT: steps of eight heads.  fp32: queries and weights as two halves each.
@@ -422,6 +422,7 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
     }
     float corr[NT][2];
     bool grew = false;
+    float most = -INFINITY;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -448,21 +449,30 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
           kref[n][e] = vr[n][e];
           grew = true;
         }
-        const float d = mnr - xref[n][e] - kref[n][e] + 10.f;  // (+inf while no row has had a weight: the weights are 0)
+        const float d = mnr - xref[n][e] - kref[n][e] + 10.f;
+        most = fmaxf(most, d);  // (+inf while no row has had a weight: the weights are 0)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float up = d + ve[h], f = vm[h] * ex2_approx(fminf(up, 120.f));
 #pragma unroll
           for (int q = 0; q < 2; ++q) x[n][h][q * 2 + e] *= f;
-          // Weights are 2^-126 and more and their products with f below 2^15, so up is below 142 where there are any: the
-          // part beyond an exponent's range is a second factor.
-          if (up > 120.f) {
-            const float f2 = ex2_approx(fminf(up, 142.f) - 120.f);
+        }
+      }
+    // Weights are 2^-126 and more and their products with f below 2^15, so the exponent of f is below 142 where there are
+    // any: what is beyond its range is a second factor.
+    if (most + fmaxf(ve[0], ve[1]) > 120.f) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float up = (mrow[n][e] == -INFINITY ? 0.f : mrow[n][e]) - xref[n][e] - kref[n][e] + 10.f + ve[h];
+            const float f2 = ex2_approx(fminf(fmaxf(up - 120.f, 0.f), 22.f));
 #pragma unroll
             for (int q = 0; q < 2; ++q) x[n][h][q * 2 + e] *= f2;
           }
-        }
-      }
+    }
     if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -576,13 +586,17 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) M = fmaxf(M, wm[w][hd]);
       const bool none = mrow[n][e] == -INFINITY;  // this warp has no row with a weight
-      // (two factors where one would be below 2^-126: a weight may be that small, and its row's scale too)
       const float down = (xref[n][e] - M) + (kref[n][e] - 10.f);
-      const float f = none ? 0.f : ex2_approx(fmaxf(down, -100.f)), f2 = down < -100.f ? ex2_approx(down + 100.f) : 1.f;
+      const float f = none ? 0.f : ex2_approx(fmaxf(down, -100.f));
+      if (down < -100.f) {  // two factors where one may be below 2^-126: a weight is as small as that, and a row's scale too
+        const float f2 = ex2_approx(down + 100.f);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[n][c][e] *= f2, o[n][c][2 + e] *= f2;
+      }
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         *reinterpret_cast<float2*>(wo + (warp * GU + hd) * C::kFoldLd + c * 16 + 2 * g) =
-            make_float2(o[n][c][e] * f * f2, o[n][c][2 + e] * f * f2);
+            make_float2(o[n][c][e] * f, o[n][c][2 + e] * f);
       if (g == 0) {
         wl[warp][hd] = none ? lrow[n][e] : lrow[n][e] * ex2_approx(mrow[n][e] - M);
         if (warp == 0) s_M[hd] = M;
