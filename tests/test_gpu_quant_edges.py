@@ -1,6 +1,7 @@
 """Caches held in 8 bits at their edges, against the plain form in 64 bits: workspaces that go from one cache to
 another, weights far below the largest, a NaN among the compensation, scales of the caller's own
-below the smallest fresh one."""
+below the smallest fresh one, rows read back and decoded over at once, and fp32 decodes held to a limit that tells queries and
+weights in two halves from one."""
 import math
 
 import numpy as np
@@ -9,6 +10,7 @@ import torch
 
 import paper_2607_16213_gb300 as S
 from paper_2607_16213_gb300 import api
+import quant_fine as F
 import quant_ref as R
 from test_gpu_quant import Model, TORCH, filled, gen, make, np64, rows, u8
 
@@ -228,3 +230,26 @@ def test_the_kernel_in_front_of_a_decode_writes_no_rows(graph):
     for i in range(12):
         assert torch.equal(outs[i], want[i % 3]), i
     assert ws.errors() == 0 and wr.errors() == 0
+
+
+# ---- fp32 caches: both halves count ---------------------------------------------------------------------
+@pytest.mark.parametrize("case", F.CASES)
+@pytest.mark.parametrize("seed", [1, 2])
+def test_fp32_decode_to_its_last_digits(case, seed):
+    """Unit rows and queries (F says what a result may be off; the host test beside it that one half would not do)."""
+    d, hq, hkv, lens, kind, block = case
+    q, k, v, bias = (torch.from_numpy(x).cuda() for x in F.inputs(case, seed))
+    B, n = len(lens), max(lens)
+    c = make("fp32", B, hq, hkv, d, n + 5, kind, block)
+    api.quant_append(c, k, v, bias, torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    model = Model(c)
+    out = np64(api.decode_quant(c, q)).reshape(B, hkv, hq // hkv, d)
+    worst = 0.0
+    for b in range(B):
+        for h in range(hkv):
+            kk, vv = model.head(b, h)
+            np.testing.assert_array_equal(kk, F.cached(np64(k)[b, h], lens[b], kind, block)[0])
+            want, lim = F.limit(np64(q)[b].reshape(hkv, -1, d)[h], kk, vv, model.bias[b, h, :lens[b]])
+            worst = max(worst, float((np.abs(out[b, h] - want) / lim).max()))
+    print("largest error over its limit: %.3f" % worst)
+    assert worst <= 1
