@@ -298,17 +298,20 @@ SELKV_API selkv_status selkv_layer_average_bias(const selkv_shape* shape, const 
  * An empty cache with no new row gives out = 0.  An append that would pass m_cap is skipped
  * and sets SELKV_DEVERR_CAPACITY.
  *
+ * The workspace's counters and partials lie where B and Hkv put them: one that has served another call,
+ * or a decode of other B or Hkv, is zeroed (selkv_workspace_init) before it serves this one.
+ *
  * Overlap with the previous kernel (bf16 caches): the decode is launched with programmatic
  * dependent launch and may start loading cache rows below lengths[b] - 1 while the kernel
  * enqueued just before it on the same stream is still running.  That kernel must therefore
  * not write those rows of K_c and V_c (it may write q, k_new, v_new, the bias, lengths, and
  * row lengths[b] - 1 onwards).  The library's own calls never do: a decode appends only at
  * lengths[b], and a compression and a selkv_qcache_read write their rows before their last
- * kernel.  A caller kernel
- * that rewrites cached rows must be separated from the decode by another stream operation
- * (any other kernel, a copy or an event).  Everything the result is computed from is read
- * after the previous kernel has completed: rows loaded early are used only where the slice
- * planned from the final lengths[b] starts at the same row and covers them.
+ * kernel.  A caller kernel that rewrites cached rows must be separated from the decode by
+ * another stream operation (any other kernel, a copy or an event).  Everything the result is
+ * computed from is read after the previous kernel has completed: rows loaded early are used
+ * only where the slice planned from the final lengths[b] starts at the same row and covers
+ * them.
  * ------------------------------------------------------------------------------------- */
 SELKV_API size_t selkv_decode_workspace_size(const selkv_shape* shape);
 
@@ -424,11 +427,13 @@ SELKV_API selkv_status selkv_qcache_read(const selkv_shape* shape, const selkv_q
  * gives out = 0, as does an empty cache without a new row; rows whose bias is the lowest finite
  * number are the limit of very small weights (rows that all have it share the weight); weights below 2^-126
  * of the largest count as none; a row whose bias is NaN makes its heads' outputs NaN.  Without a cache's
- * bias (NULL) none is read and none is written.  An append that would pass m_cap is skipped and sets
- * SELKV_DEVERR_CAPACITY (the output has no new row then).
- * Workspaces: initialised once with selkv_workspace_init, one serves selkv_qcache_append, selkv_qcache_read and this call over any
- * caches, one after another, that it is large enough for (a decode's size counts its partials and is enough
- * for the other two; 0 for a shape that no cache has).
+ * bias (NULL) none is read and none is written.  Sums are held in fp32 until they are divided by the sum of
+ * the weights (as in selkv_decode_attn): values above 3.4e38 / L may give infinities.  An append that would
+ * pass m_cap is skipped and sets SELKV_DEVERR_CAPACITY (the output has no new row then).
+ * Workspaces: initialised once with selkv_workspace_init, one serves selkv_qcache_append, selkv_qcache_read and
+ * this call over any caches, one after another, that it is large enough for (a decode's size counts its
+ * partials and is enough for the other two; 0 for a shape that no cache has).  One that has served other
+ * calls than these three is zeroed first.
  * Errors as selkv_decode_attn; SELKV_ERR_UNSUPPORTED also when B Hkv m_cap >= 2^31. */
 SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);
 

@@ -22,6 +22,8 @@ namespace selkv {
 // The constants below were fitted to the times of all plans (caches larger than L2, a row appended) for 744 batches:
 // 1 to 1024 heads, 90 to 130000 rows, 1 to 16 query heads, d 64 and 128, both types, full and ragged.  The plan that
 // they choose takes 0.9 percent more than the best one on average and 15 percent at most; of 80 other batches 1.7 and 12.
+// (The caches were full to within 100 rows of m_cap, or ragged from a half up: the split follows m_cap, not the lengths,
+// so that shorter ones are split further than they need.)
 namespace {
 double plan_us(const selkv_shape& s, int warps, int S, int cluster) {
   const bool wide = s.num_q_heads / s.num_kv_heads > 8, fp32 = s.dtype == SELKV_FP32;

@@ -20,12 +20,16 @@
 // weights p = 2^(x - largest x so far) are summed in fp32, and go into O as
 //   fp16(p * vs * 2^(largest x so far - ref)),
 // ref a reference that only grows and keeps these below 2^15: the scales of V never meet O, and
-// weights down to 2^-24 of the largest keep 11 bits (fp32 caches: 22, as two halves).
+// weights (times their scales) down to 2^-24 of the largest keep 11 bits.  fp32 caches hold them as two halves: 22 bits down
+// to 2^-12 of the largest, and an error of at most 2^-35 of the largest below that.
 //
-// A key row costs 2 d + 4 bytes of HBM and 4 G d flops.  What bounds it: HBM from some tens of MB on
-// (131072 x 8 rows of d 128, 269 MB: 44.7 us, 6.0 TB/s of 6.8 measured for a copy); below that the way in
-// (length, queries and the first tiles: 3 us) and out (fold of warps and splits: 2 to 4 us); for d 64
-// the work of a tile, which is that of d 128 but for half of the products.
+// A key row costs 2 d + 4 bytes of HBM and 4 G d flops.  What bounds it: for bf16, d 128 and up to eight heads a group HBM
+// from some tens of MB on (131072 x 8 rows, 269 MB: 45.2 us, 5.9 TB/s of 6.8 measured for a copy); below that the way in
+// (length, queries and the first tiles: 3 us) and out (fold of warps and splits: 2 to 4 us).  The other forms are
+// bound by the instructions of a tile (floor 39 to 40 us each; 8 caches of 16000 x 8 rows of d 128 or 32000 x 8 of d 64, fp32 d 128
+// 4 of 32000 x 8): d 64, whose tile costs as d 128's but for half of the products, 48 to 51 us; nine to sixteen heads, whose
+// registers leave room for eight to twelve warps on an SM, 54 to 77; fp32, with each product twice, 50 to 67, and 78 to 94
+// with both.
 #pragma once
 
 #include "decode_common.cuh"
@@ -337,7 +341,8 @@ __global__ __launch_bounds__(NW * 32, ctas_of(NW, NT == 2, sizeof(T) == 4, D)) v
     // S^T = K Q^T: the bytes 4 j .. 4 j + 3 of chunk c are the k indexes 2 j, 2 j + 1, 2 j + 8, 2 j + 9 of step c
     // (The tensor cores cut sums off instead of rounding them.  With fp32 caches the products with the second halves
     // of the queries therefore have sums of their own here, and a tile's share of O is added to it below: errors of
-    // 2e-7 to 6e-7 of the output instead of 2e-7 to 1.3e-6.)
+    // 2e-7 to 6e-7 of the output instead of 2e-7 to 1.3e-6.  Many equal rows near 2^-24 of the largest weight would all be
+    // rounded the same way: 100000 of them to some 3e-6 of the output.)
     float x[NT][2][4], x2[NT][2][4] = {};  // heads n * 8 + 2 j + (i & 1), rows 16 h + 8 (i >> 1) + g
 #pragma unroll
     for (int n = 0; n < NT; ++n)

@@ -163,9 +163,8 @@ struct QDecodePlan {
   int warps, splits, cluster;
 };
 QDecodePlan decode_q_plan(const selkv_shape& s);
-// CTA sizes: few (sequence, KV head) pairs get large CTAs, one on an SM (few splits to fold); many get
-// small ones.
-// CTAs on an SM, as registers allow (wide: more than eight heads).
+// CTA sizes: few (sequence, KV head) pairs get large CTAs, one or two on an SM (few splits to fold); many get small
+// ones.  CTAs on an SM, as registers allow (wide: more than eight heads).
 constexpr int kMaxQCtas = 4;
 constexpr int ctas_of(int warps, bool wide, bool fp32, int d) {
   if (!wide && !fp32) return warps == 8 ? 2 : kMaxQCtas;
