@@ -253,3 +253,60 @@ def test_fp32_decode_to_its_last_digits(case, seed):
             worst = max(worst, float((np.abs(out[b, h] - want) / lim).max()))
     print("largest error over its limit: %.3f" % worst)
     assert worst <= 1
+
+
+# ---- the most sequences, and streams by their handles ---------------------------------------------------
+@pytest.mark.parametrize("kind,d", [("e4m3", 64), ("int8", 128)])
+def test_the_most_sequences_and_heads(kind, d):
+    """1024 sequences of 32 KV heads on one workspace: appended to, decoded over with a new row, read back."""
+    B, hkv, cap = 1024, 32, 50
+    c = make("bf16", B, hkv, hkv, d, cap, kind, 16)
+    g = gen(d)
+    k, v = rows(g, B, hkv, 40, d, "bf16", loud=False), rows(g, B, hkv, 40, d, "bf16", loud=False)
+    counts = (torch.arange(B, dtype=torch.int32, device="cuda") * 7) % 41
+    ws = api.Workspace(S.selkv_decode_q_workspace_size(c.shape))
+    api.quant_append(c, k, v, counts=counts, workspace=ws)
+    assert torch.equal(c.lengths, counts)
+    K, V = (x.double() for x in api.quant_read(c, 0, 41, workspace=ws))
+    q = torch.randn((B, hkv, d), generator=g, device="cuda").bfloat16()
+    kn, vn = (torch.randn((B, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    out = api.decode_quant(c, q, kn, vn, workspace=ws)
+    assert torch.equal(c.lengths, counts + 1) and ws.errors() == 0
+    at = counts.long()[:, None, None, None].expand(B, hkv, 1, d)
+    K.scatter_(2, at, kn.double()[:, :, None])
+    V.scatter_(2, at, vn.double()[:, :, None])
+    s = (q.double()[:, :, None] * K).sum(3) / math.sqrt(d)
+    s.masked_fill_(torch.arange(41, device="cuda") > counts[:, None, None], -math.inf)
+    p = torch.softmax(s, 2)
+    want = (p[..., None] * V).sum(2)
+    # The rows read back in bf16 are off by 2^-8 of themselves (int8 codes times four bits; e4m3 exactly): of a key that moves
+    # a logit by 2^-8 sum |q k| / sqrt(d), and a weight and the normaliser by e to that.  The kernel: weights 2^-11, logits and sums
+    # far below 2^-11; the output 2^-8.
+    read = 2.0 ** -8 if kind == "int8" else 0.0
+    mag = (q.double().abs()[:, :, None] * K.abs()).sum(3).amax(2) / math.sqrt(d)
+    pv = (p[..., None] * V.abs()).sum(2)
+    lim = ((read + torch.expm1(2 * read * mag))[..., None] + 2.0 ** -11 + 2.0 ** -11 * (1 + mag)[..., None]) * pv + 2.0 ** -8 * want.abs() + 1e-30
+    assert bool(((out.double() - want).abs() <= lim).all())
+
+
+def test_streams_by_handle_and_object():
+    """Every call takes a stream as its handle (0: the default one) or as an object."""
+    c, g = filled("bf16", 2, 8, 2, 128, 300, "e4m3", 64, [250, 30], 12)
+    model = Model(c)
+    q = torch.randn((2, 8, 128), generator=g, device="cuda").bfloat16()
+    want = api.decode_quant(c, q)
+    torch.cuda.synchronize()
+    for stream in (0, torch.cuda.default_stream(), torch.cuda.Stream(), torch.cuda.Stream().cuda_stream):
+        k, v = rows(g, 2, 2, 3, 128, "bf16"), rows(g, 2, 2, 3, 128, "bf16")
+        torch.cuda.synchronize()
+        out = api.decode_quant(c, q, stream=stream)
+        K, _ = api.quant_read(c, 0, 30, stream=stream)
+        api.quant_append(c, k, v, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        for b in range(2):
+            assert torch.equal(K[b, 1].cpu(), torch.from_numpy(model.head(b, 1)[0][:30]).bfloat16())
+        model.append(k, v, [3, 3])
+        model.check()
+        want = api.decode_quant(c, q)
+        torch.cuda.synchronize()
