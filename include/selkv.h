@@ -106,7 +106,9 @@ typedef enum selkv_rope {
 #define SELKV_DEVERR_TIMEOUT 0x2u  /* a bounded wait gave up; the launch's output is void  */
 #define SELKV_DEVERR_LENGTH 0x4u   /* lengths[b] outside [0, m_cap]; clamped              */
 #define SELKV_DEVERR_COUNT 0x8u    /* compress kept a count other than m_b (internal)     */
-#define SELKV_DEVERR_VALUE 0x10u   /* an infinity or NaN was put into an 8-bit cache       */
+#define SELKV_DEVERR_VALUE 0x10u   /* an infinity or NaN was put into an 8-bit cache; a number given to
+                                      selkv_tree_verify is no probability, no token or not in [0, 1)  */
+#define SELKV_DEVERR_TREE 0x20u    /* a parent or path entry is no token of the tree        */
 
 typedef struct selkv_shape {
   int32_t dtype;        /* selkv_dtype of K, V, Q_obs, q, k_new, v_new, K_c, V_c and out  */
@@ -440,6 +442,158 @@ SELKV_API size_t selkv_decode_q_workspace_size(const selkv_shape* shape);
 SELKV_API selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* cache, const void* q,
                                            const void* k_new, const void* v_new, void* out, void* workspace,
                                            size_t workspace_bytes, selkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Rotary positions of queries and keys.  The caller of a decode embeds its new queries and keys
+ * (see selkv_rope); this does it, for one token or a whole prompt: of the first rot_dim elements of a
+ * row, pair f in [0, rot_dim / 2) at position p becomes
+ *   y0 = amplitude (x0 cos(p w_f) - x1 sin(p w_f)),   y1 = amplitude (x1 cos(p w_f) + x0 sin(p w_f)),
+ * the pair (x[f], x[f + rot_dim / 2]) (HALF layout) or (x[2f], x[2f + 1]) (INTERLEAVED); the elements
+ * behind rot_dim stay.  w_f = theta^(-2f / rot_dim) radians a position, for long contexts scaled:
+ *   LINEAR      w_f / factor;
+ *   WAVELENGTH  k_f w_f + (1 - k_f) w_f / factor, with k_f = (turns_f - low) / (high - low) clamped to [0, 1]
+ *               and turns_f = original w_f / (2 pi) the turns of the pair over the original context;
+ *   RAMP        the same with k_f = 1 - (f - i0) / (i1 - i0) clamped, i0 = max(0, floor(c(high))),
+ *               i1 = min(rot_dim - 1, ceil(c(low))), c(n) = rot_dim ln(original / (2 pi n)) / (2 ln theta)
+ *               (i1 - i0 at least 0.001).
+ * Angles are taken in turns in 64-bit fixed point (their wrap is the reduction): right to 2^-33 turns for every
+ * 32-bit position; sine, cosine and products in fp32, one rounding to the dtype at the end.
+ * ------------------------------------------------------------------------------------- */
+typedef enum selkv_rope_scale {
+  SELKV_ROPE_SCALE_NONE = 0,
+  SELKV_ROPE_SCALE_LINEAR = 1,
+  SELKV_ROPE_SCALE_WAVELENGTH = 2,
+  SELKV_ROPE_SCALE_RAMP = 3
+} selkv_rope_scale;
+
+typedef struct selkv_rope_scaling {
+  int32_t kind;     /* selkv_rope_scale                                                           */
+  int32_t original; /* positions of the original context, at least 1 (WAVELENGTH, RAMP)           */
+  double factor;    /* finite, > 0                                                                */
+  double low, high; /* turns over the original context, 0 < low < high (WAVELENGTH, RAMP)         */
+  double amplitude; /* finite, > 0; 0: 1, for RAMP 0.1 ln(factor) + 1 (factor > 1)                */
+} selkv_rope_scaling;
+
+#define SELKV_ROTARY_MAX_DIM 128
+
+/* A plan on the host: filled once by selkv_rotary_init, read by every call (and copied by it). */
+typedef struct selkv_rotary {
+  int32_t layout;  /* SELKV_ROPE_HALF or SELKV_ROPE_INTERLEAVED                                   */
+  int32_t rot_dim; /* even, 2 .. SELKV_ROTARY_MAX_DIM                                             */
+  float amplitude;
+  int32_t reserved;
+  uint64_t turns[SELKV_ROTARY_MAX_DIM / 2]; /* w_f / (2 pi) 2^64, modulo 2^64                     */
+} selkv_rotary;
+
+/* scaling may be NULL (none).  SELKV_ERR_INVALID_ARG for a layout, dimension, theta (finite, > 0; > 1 for RAMP) or
+ * scaling outside the rules above.  Host only. */
+SELKV_API selkv_status selkv_rotary_init(selkv_rotary* plan, int32_t rot_dim, int32_t layout, double theta,
+                                         const selkv_rope_scaling* scaling);
+
+/* q, q_out   [B][Hq][tokens][d] of the shape's dtype, both or neither; k, k_out [B][Hkv][tokens][d], both or
+ *            neither.  An output may be its input (in place), and overlaps nothing else.
+ * positions  [B][tokens] int32 device, any value.
+ * transpose  nonzero: the rotations' transposes (sine negated): takes positions off again where the amplitude
+ *            is 1, and is the gradient of the call without it.
+ * SELKV_ERR_UNSUPPORTED for d not in {64, 128}; SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor, neither q
+ * nor k, tokens below 1, a plan that selkv_rotary_init did not fill or whose rot_dim is above d.  No workspace. */
+SELKV_API selkv_status selkv_rotary_apply(const selkv_shape* shape, const selkv_rotary* plan, int32_t tokens,
+                                          const int32_t* positions, const void* q, const void* k, void* q_out,
+                                          void* k_out, int32_t transpose, selkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * A tree of drafted tokens over a cache.  A model that drafts several tokens scores them in one pass over the
+ * cache (selkv_tree_attn, per layer), keeps the ones that its probabilities bear out
+ * (selkv_tree_verify) and puts their rows into the caches (selkv_tree_commit).
+ *
+ * tokens    T tokens a sequence, 1 .. SELKV_MAX_TREE.
+ * parents   [B][T] int32 device: -1, or a token before it (parents[t] < t), or NULL: a chain (t - 1).
+ *           Token 0 is the last certain one, whose row is not in the cache yet; its parent is -1.
+ * counts    [B] int32 device, 0 .. T: tokens that sequence b has, or NULL: T.
+ * A parent outside [-1, t) counts as -1 and sets SELKV_DEVERR_TREE; a count out of range is clamped and sets
+ * SELKV_DEVERR_LENGTH.
+ * ------------------------------------------------------------------------------------- */
+#define SELKV_MAX_TREE 128
+
+typedef struct selkv_tree {
+  int32_t tokens;
+  const int32_t* parents;
+  const int32_t* counts;
+} selkv_tree;
+
+/* Compensated attention of a tree's tokens: token t < counts[b] of query head h sees the L = lengths[b] cached
+ * rows, its ancestors and itself,
+ *   out[b][h][t] = sum_i p_i V_c[b][kv][i] + sum_u p_u v_new[b][kv][u],   p = softmax over i < L of
+ *                  q . K_c[b][kv][i] / sqrt(d) + bias[b][kv][i]  and over u in {t, its ancestors} of
+ *                  q . k_new[b][kv][u] / sqrt(d).
+ * Nothing is appended: the cache and lengths stay.
+ *
+ * q, out        [B][Hq][T][d] of the shape's dtype; outputs of tokens at or behind counts[b] are left as they were.
+ * k_new, v_new  [B][Hkv][T][d] of the shape's dtype; rows at or behind counts[b] are not used.
+ * K_c, V_c, bias, lengths  as in selkv_decode_attn (bias may be NULL; a length out of range is clamped and sets
+ *               SELKV_DEVERR_LENGTH).
+ * A row whose bias is -inf has no weight, whatever it holds, and so have the rows of tokens that t does not see; a
+ * NaN in the bias or a logit reaches its tokens' outputs.  bf16: weights relative to the largest are rounded to bf16
+ * before they meet the values, sums are held in fp32.
+ * Errors as selkv_decode_attn, and SELKV_ERR_INVALID_ARG for a tree outside the rules above;
+ * SELKV_ERR_UNSUPPORTED also for B Hkv m_cap >= 2^31.  The workspace is initialised once (selkv_workspace_init); one
+ * serves selkv_tree_attn, selkv_tree_verify and selkv_tree_commit of any shapes, one after another, that it is large
+ * enough for.  Sizes are 0 for shapes that no call takes. */
+SELKV_API size_t selkv_tree_attn_workspace_size(const selkv_shape* shape, int32_t tokens);
+
+SELKV_API selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tree* tree, const void* q, const void* K_c,
+                                       const void* V_c, const float* bias, const int32_t* lengths, const void* k_new,
+                                       const void* v_new, void* out, void* workspace, size_t workspace_bytes,
+                                       selkv_stream_t stream);
+
+/* Verification of a tree's tokens against the target's probabilities, from given random numbers: a walk from
+ * token 0.  At a node with target distribution p (what follows it) and, if its children were drawn,
+ * draft distribution q, the weights start as r = p with mass M = 1, and the node's children are tried in order of
+ * their index.  Child t with token x is accepted, and becomes the node, where
+ *   uniforms[t] M q(x) < r(x);          otherwise r <- max(r - M q, 0) and M <- sum r;
+ * with draft = NULL (children picked without drawing, for instance the most likely ones)
+ *   uniforms[t] M < r(x);               otherwise r(x) <- 0 and M <- M - r(x) (of the old r(x)).
+ * (A rejection that would leave M <= 0 leaves r and M as they are.)  Where no child is left the next token is drawn
+ * from r: the smallest x with r(0) + .. + r(x) > uniforms[0] (sum r), or vocab - 1 where r has no mass.  Children drawn
+ * independently from q (or picked) leave tokens distributed as the target's own.
+ *
+ * tokens    [B][T] int32 device, in [0, vocab) (token 0's is not read).
+ * uniforms  [B][T] fp32 device, in [0, 1): entry t > 0 decides on token t, entry 0 draws the next token.
+ * target    [B][T][vocab] fp32 device: row t the probabilities of what follows token t; draft the same or NULL.
+ * accepted  [B] int32 output: tokens of the path, token 0 among them (0 for a sequence without tokens).
+ * path      [B][T] int32 output: their indices in order, -1 behind them.
+ * next_token  [B] int32 output (-1 for a sequence without tokens).
+ * Weights are held in 64-bit fixed point (units of 2^-62) and their sums are exact: results do not depend on the order of
+ * additions.  A probability that is NaN, negative or at least 2 counts as 0, a token outside the vocabulary is never accepted,
+ * a uniform outside [0, 1) is clamped (NaN: 0); each sets SELKV_DEVERR_VALUE where the call meets it.
+ * batch 1 .. SELKV_MAX_BATCH, vocab 1 .. 2^20.  Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor
+ * (draft may be NULL) or a size out of range; SELKV_ERR_WORKSPACE as elsewhere. */
+SELKV_API size_t selkv_tree_verify_workspace_size(int32_t batch, int32_t tokens, int32_t vocab);
+
+SELKV_API selkv_status selkv_tree_verify(int32_t batch, const selkv_tree* tree, int32_t vocab, const int32_t* tokens,
+                                         const float* uniforms, const float* target, const float* draft,
+                                         int32_t* accepted, int32_t* path, int32_t* next_token, void* workspace,
+                                         size_t workspace_bytes, selkv_stream_t stream);
+
+/* The accepted rows into the caches of a model's layers: for every layer and sequence, row path[b][i] of K_new and
+ * V_new, i < accepted[b], goes to row lengths[b] + i of the layer's cache with bias 0, and lengths[b] += accepted[b].
+ *
+ * num_layers  1 .. 128.
+ * tokens      T of K_new, V_new [B][Hkv][T][d] and of path.
+ * path [B][T], accepted [B]  int32 device, as selkv_tree_verify leaves them.
+ * K_new, V_new, K_c, V_c, lengths  HOST arrays [num_layers] of device pointers; bias the same, or NULL, or with NULL
+ *             entries.  No layer's lengths (or cache) are another one's.
+ * A sequence whose rows would pass m_cap takes none of them in that layer and sets SELKV_DEVERR_CAPACITY; one with a path
+ * entry outside [0, T) takes none at all and sets SELKV_DEVERR_TREE; accepted outside [0, T] or a length out of range is
+ * clamped and sets SELKV_DEVERR_LENGTH.  A selkv_decode_attn may follow at once (the call's last kernel writes no rows).
+ * Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor, sizes out of range or lengths given twice;
+ * SELKV_ERR_UNSUPPORTED for d not in {64, 128}; SELKV_ERR_WORKSPACE as elsewhere. */
+SELKV_API size_t selkv_tree_commit_workspace_size(const selkv_shape* shape);
+
+SELKV_API selkv_status selkv_tree_commit(const selkv_shape* shape, int32_t num_layers, int32_t tokens, const int32_t* path,
+                                         const int32_t* accepted, const void* const* K_new, const void* const* V_new,
+                                         void* const* K_c, void* const* V_c, float* const* bias, int32_t* const* lengths,
+                                         void* workspace, size_t workspace_bytes, selkv_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -25,4 +25,8 @@ from ._binding import (  # noqa: F401
     SELKV_Q_E4M3, SELKV_Q_INT8, SELKV_DEVERR_VALUE, selkv_qcache, selkv_qcache_workspace_size, selkv_qcache_append,
     selkv_qcache_read, selkv_decode_q_workspace_size, selkv_decode_attn_q,
     SELKV_STATIC_SCRATCH_BYTES,
+    SELKV_DEVERR_TREE, SELKV_ROPE_SCALE_NONE, SELKV_ROPE_SCALE_LINEAR, SELKV_ROPE_SCALE_WAVELENGTH, SELKV_ROPE_SCALE_RAMP,
+    SELKV_ROTARY_MAX_DIM, SELKV_MAX_TREE, selkv_rope_scaling, selkv_rotary, selkv_tree, selkv_rotary_init, selkv_rotary_apply,
+    selkv_tree_attn_workspace_size, selkv_tree_attn, selkv_tree_verify_workspace_size, selkv_tree_verify,
+    selkv_tree_commit_workspace_size, selkv_tree_commit,
 )

@@ -20,7 +20,10 @@ SELKV_BIAS_RATIO, SELKV_BIAS_COUNT = 0, 1
 SELKV_ROUTE_BUCKET, SELKV_ROUTE_COSINE = 0, 1
 SELKV_SCORE_ROWSTATS, SELKV_SCORE_COLSUMS, SELKV_SCORE_ALL = 1, 2, 3
 SELKV_DEVERR_CAPACITY, SELKV_DEVERR_TIMEOUT, SELKV_DEVERR_LENGTH, SELKV_DEVERR_COUNT = 1, 2, 4, 8
-SELKV_DEVERR_VALUE = 16
+SELKV_DEVERR_VALUE, SELKV_DEVERR_TREE = 16, 32
+SELKV_ROPE_SCALE_NONE, SELKV_ROPE_SCALE_LINEAR, SELKV_ROPE_SCALE_WAVELENGTH, SELKV_ROPE_SCALE_RAMP = 0, 1, 2, 3
+SELKV_ROTARY_MAX_DIM = 128
+SELKV_MAX_TREE = 128
 SELKV_Q_E4M3, SELKV_Q_INT8 = 0, 1
 SELKV_MAX_BATCH = 1024
 SELKV_STATIC_SCRATCH_BYTES = 4 << 20
@@ -72,6 +75,20 @@ class selkv_qcache(ctypes.Structure):
                 ("V_scale", c_vp), ("bias", c_vp), ("lengths", c_vp)]
 
 
+class selkv_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", c_i32), ("original", c_i32), ("factor", c_f64), ("low", c_f64), ("high", c_f64),
+                ("amplitude", c_f64)]
+
+
+class selkv_rotary(ctypes.Structure):
+    _fields_ = [("layout", c_i32), ("rot_dim", c_i32), ("amplitude", c_f32), ("reserved", c_i32),
+                ("turns", c_u64 * (SELKV_ROTARY_MAX_DIM // 2))]
+
+
+class selkv_tree(ctypes.Structure):
+    _fields_ = [("tokens", c_i32), ("parents", c_vp), ("counts", c_vp)]
+
+
 _LIB: Optional[ctypes.CDLL] = None
 
 
@@ -119,6 +136,17 @@ def library() -> ctypes.CDLL:
         "selkv_decode_q_workspace_size": (c_sz, [ctypes.POINTER(selkv_shape)]),
         "selkv_decode_attn_q": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_qcache), c_vp, c_vp,
                                         c_vp, c_vp, c_vp, c_sz, c_vp]),
+        "selkv_rotary_init": (c_i32, [ctypes.POINTER(selkv_rotary), c_i32, c_i32, c_f64,
+                                      ctypes.POINTER(selkv_rope_scaling)]),
+        "selkv_rotary_apply": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_rotary), c_i32, c_vp, c_vp,
+                                       c_vp, c_vp, c_vp, c_i32, c_vp]),
+        "selkv_tree_attn_workspace_size": (c_sz, [ctypes.POINTER(selkv_shape), c_i32]),
+        "selkv_tree_attn": (c_i32, [ctypes.POINTER(selkv_shape), ctypes.POINTER(selkv_tree)] + [c_vp] * 9 + [c_sz, c_vp]),
+        "selkv_tree_verify_workspace_size": (c_sz, [c_i32, c_i32, c_i32]),
+        "selkv_tree_verify": (c_i32, [c_i32, ctypes.POINTER(selkv_tree), c_i32] + [c_vp] * 8 + [c_sz, c_vp]),
+        "selkv_tree_commit_workspace_size": (c_sz, [ctypes.POINTER(selkv_shape)]),
+        "selkv_tree_commit": (c_i32, [ctypes.POINTER(selkv_shape), c_i32, c_i32, c_vp, c_vp] +
+                              [ctypes.POINTER(c_vp)] * 6 + [c_vp, c_sz, c_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -283,3 +311,64 @@ def selkv_decode_attn_q(shape: selkv_shape, cache: selkv_qcache, q, k_new, v_new
     return library().selkv_decode_attn_q(ctypes.byref(shape), ctypes.byref(cache), _ptr(q), _ptr(k_new),
                                          _ptr(v_new), _ptr(out), _ptr(workspace), int(workspace_bytes),
                                          _stream(stream))
+
+
+def selkv_rotary_init(plan: selkv_rotary, rot_dim: int, layout: int, theta: float, scaling=None) -> int:
+    """See include/selkv.h (host only)."""
+    return library().selkv_rotary_init(ctypes.byref(plan), int(rot_dim), int(layout), float(theta),
+                                       ctypes.byref(scaling) if scaling is not None else None)
+
+
+def selkv_rotary_apply(shape: selkv_shape, plan: selkv_rotary, tokens: int, positions, q, k, q_out, k_out,
+                       transpose: int = 0, stream=None) -> int:
+    """See include/selkv.h."""
+    return library().selkv_rotary_apply(ctypes.byref(shape), ctypes.byref(plan), int(tokens), _ptr(positions), _ptr(q),
+                                        _ptr(k), _ptr(q_out), _ptr(k_out), int(transpose), _stream(stream))
+
+
+def _tree(tokens: int, parents, counts) -> selkv_tree:
+    return selkv_tree(int(tokens), _ptr(parents), _ptr(counts))
+
+
+def selkv_tree_attn_workspace_size(shape: selkv_shape, tokens: int) -> int:
+    return int(library().selkv_tree_attn_workspace_size(ctypes.byref(shape), int(tokens)))
+
+
+def selkv_tree_attn(shape: selkv_shape, tokens: int, parents, counts, q, K_c, V_c, bias, lengths, k_new, v_new, out,
+                    workspace, workspace_bytes: int, stream=None) -> int:
+    """See include/selkv.h (tokens, parents and counts: the selkv_tree)."""
+    return library().selkv_tree_attn(ctypes.byref(shape), ctypes.byref(_tree(tokens, parents, counts)), _ptr(q),
+                                     _ptr(K_c), _ptr(V_c), _ptr(bias), _ptr(lengths), _ptr(k_new), _ptr(v_new),
+                                     _ptr(out), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def selkv_tree_verify_workspace_size(batch: int, tokens: int, vocab: int) -> int:
+    return int(library().selkv_tree_verify_workspace_size(int(batch), int(tokens), int(vocab)))
+
+
+def selkv_tree_verify(batch: int, num_tokens: int, parents, counts, vocab: int, tokens, uniforms, target, draft, accepted,
+                      path, next_token, workspace, workspace_bytes: int, stream=None) -> int:
+    """See include/selkv.h (num_tokens, parents and counts: the selkv_tree)."""
+    return library().selkv_tree_verify(int(batch), ctypes.byref(_tree(num_tokens, parents, counts)), int(vocab),
+                                       _ptr(tokens), _ptr(uniforms), _ptr(target), _ptr(draft), _ptr(accepted),
+                                       _ptr(path), _ptr(next_token), _ptr(workspace), int(workspace_bytes),
+                                       _stream(stream))
+
+
+def selkv_tree_commit_workspace_size(shape: selkv_shape) -> int:
+    return int(library().selkv_tree_commit_workspace_size(ctypes.byref(shape)))
+
+
+def selkv_tree_commit(shape: selkv_shape, tokens: int, path, accepted, K_new, V_new, K_c, V_c, bias, lengths, workspace,
+                      workspace_bytes: int, stream=None) -> int:
+    """K_new, V_new, K_c, V_c, lengths: sequences of per-layer tensors (or device addresses); bias too, or None,
+    or with entries None."""
+    L = len(K_new)
+    if not all(len(x) == L for x in (V_new, K_c, V_c, lengths)) or (bias is not None and len(bias) != L):
+        return SELKV_ERR_INVALID_ARG
+
+    def table(x):
+        return (c_vp * max(1, L))(*[_ptr(t) for t in x])
+    return library().selkv_tree_commit(ctypes.byref(shape), L, int(tokens), _ptr(path), _ptr(accepted), table(K_new),
+                                       table(V_new), table(K_c), table(V_c), table(bias) if bias is not None else None,
+                                       table(lengths), _ptr(workspace), int(workspace_bytes), _stream(stream))

@@ -296,3 +296,164 @@ def decode_quant(cache: QuantCache, q: torch.Tensor, k_new: Optional[torch.Tenso
     B.check(B.selkv_decode_attn_q(s, cache._bias if use_bias else cache._plain, q, k_new, v_new, out, ws.buf, ws.nbytes, st),
             "selkv_decode_attn_q")
     return out
+
+
+# ---- a tree of drafted tokens over a cache ------------------------------------------------------
+_SCALING = {None: B.SELKV_ROPE_SCALE_NONE, "linear": B.SELKV_ROPE_SCALE_LINEAR,
+            "wavelength": B.SELKV_ROPE_SCALE_WAVELENGTH, "ramp": B.SELKV_ROPE_SCALE_RAMP}
+_LAYOUT = {"half": B.SELKV_ROPE_HALF, "interleaved": B.SELKV_ROPE_INTERLEAVED}
+
+
+def rotary_plan(rot_dim: int, theta: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
+                factor: float = 1.0, original: int = 0, low: float = 1.0, high: float = 32.0,
+                amplitude: float = 0.0) -> B.selkv_rotary:
+    """selkv_rotary_init: the plan of a rotary embedding over the first rot_dim elements of a head, its frequencies
+    scaled for long contexts ("linear", "wavelength" or "ramp") or not (None)."""
+    if layout not in _LAYOUT or scaling not in _SCALING:
+        _bad("rotary_plan: layout is half or interleaved, scaling None, linear, wavelength or ramp")
+    plan = B.selkv_rotary()
+    how = B.selkv_rope_scaling(_SCALING[scaling], original, factor, low, high, amplitude)
+    B.check(B.selkv_rotary_init(plan, rot_dim, _LAYOUT[layout], theta, how), "selkv_rotary_init")
+    return plan
+
+
+def _cuda(t: torch.Tensor, name: str) -> torch.device:
+    if t.device.type != "cuda":
+        _bad("%s: a tensor of a CUDA device" % name)
+    return t.device
+
+
+def rotary(shape: B.selkv_shape, plan: B.selkv_rotary, positions: torch.Tensor, q: Optional[torch.Tensor] = None,
+           k: Optional[torch.Tensor] = None, out=None, transpose: bool = False, stream=None):
+    """selkv_rotary_apply: (q, k) [B][Hq or Hkv][T][d] at positions [B][T]; either may be None.  `out`: their outputs, which
+    may be the inputs themselves.  transpose: the gradient of the call without it."""
+    dev = _cuda(positions, "rotary: positions")
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return rotary(shape, plan, positions, q, k, out, transpose)
+    st = _raw_stream(dev.index)
+    if positions.dim() != 2:
+        _bad("rotary: positions [B][T]")
+    T, dt = positions.shape[1], _TORCH_DTYPE[shape.dtype]
+    _tensor(positions, "rotary: positions", (shape.batch, T), torch.int32, dev)
+    outs = list(out) if out is not None else [None, None]
+    if len(outs) != 2:
+        _bad("rotary: out is (q, k)")
+    for i, (name, x, heads) in enumerate((("q", q, shape.num_q_heads), ("k", k, shape.num_kv_heads))):
+        if x is None:
+            if outs[i] is not None:
+                _bad("rotary: an output without its input")
+            continue
+        _tensor(x, "rotary: " + name, (shape.batch, heads, T, shape.head_dim), dt, dev)
+        if outs[i] is None:
+            outs[i] = torch.empty_like(x)
+        else:
+            _tensor(outs[i], "rotary: out", x.shape, dt, dev)
+    B.check(B.selkv_rotary_apply(shape, plan, T, positions, q, k, outs[0], outs[1], transpose, st), "selkv_rotary_apply")
+    return outs[0], outs[1]
+
+
+def _tree_tensors(what: str, parents, counts, batch: int, T: int, dev) -> None:
+    if parents is not None:
+        _tensor(parents, what + ": parents", (batch, T), torch.int32, dev)
+    if counts is not None:
+        _tensor(counts, what + ": counts", (batch,), torch.int32, dev)
+
+
+def tree_attn(cache: CompressedCache, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+              parents: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None, use_bias: bool = True,
+              out: Optional[torch.Tensor] = None, workspace: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """selkv_tree_attn: a tree's tokens [B][Hq][T][d] over the cache, their ancestors and themselves (k_new, v_new
+    [B][Hkv][T][d]); parents [B][T] or None (a chain), counts [B] or None (all T).  Without `out` the outputs behind the
+    counts are zeros."""
+    s, dev = cache.shape, _cuda(cache.K_c, "tree_attn: K_c")
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return tree_attn(cache, q, k_new, v_new, parents, counts, use_bias, out, workspace)
+    st = _raw_stream(dev.index)
+    T, dt = q.shape[2] if q.dim() == 4 else 0, _TORCH_DTYPE[s.dtype]
+    want, new = (s.batch, s.num_q_heads, T, s.head_dim), (s.batch, s.num_kv_heads, T, s.head_dim)
+    rows = (s.batch, s.num_kv_heads, s.m_cap)
+    _tensor(q, "tree_attn: q", want, dt, dev)
+    _tensor(k_new, "tree_attn: k_new", new, dt, dev)
+    _tensor(v_new, "tree_attn: v_new", new, dt, dev)
+    _tensor(cache.K_c, "tree_attn: K_c", rows + (s.head_dim,), dt, dev)
+    _tensor(cache.V_c, "tree_attn: V_c", rows + (s.head_dim,), dt, dev)
+    _tensor(cache.lengths, "tree_attn: lengths", (s.batch,), torch.int32, dev)
+    bias = cache.bias if use_bias else None
+    if bias is not None:
+        _tensor(bias, "tree_attn: bias", rows, torch.float32, dev)
+    _tree_tensors("tree_attn", parents, counts, s.batch, T, dev)
+    if out is None:
+        out = torch.empty_like(q) if counts is None else torch.zeros_like(q)
+    else:
+        _tensor(out, "tree_attn: out", want, dt, dev)
+    ws = _space(workspace, lambda sh: B.selkv_tree_attn_workspace_size(sh, T), s, dev, st)
+    B.check(B.selkv_tree_attn(s, T, parents, counts, q, cache.K_c, cache.V_c, bias, cache.lengths, k_new, v_new, out, ws.buf,
+                              ws.nbytes, st), "selkv_tree_attn")
+    return out
+
+
+def tree_verify(tokens: torch.Tensor, parents: Optional[torch.Tensor], uniforms: torch.Tensor, target: torch.Tensor,
+                draft: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None, out=None,
+                workspace: Optional[Workspace] = None, stream=None):
+    """selkv_tree_verify: (accepted [B], path [B][T], next_token [B]) of trees of tokens [B][T] from the target's (and
+    the draft's) probabilities [B][T][V] and the numbers uniforms [B][T]."""
+    dev = _cuda(target, "tree_verify: target")
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return tree_verify(tokens, parents, uniforms, target, draft, counts, out, workspace)
+    st = _raw_stream(dev.index)
+    if target.dim() != 3:
+        _bad("tree_verify: target [B][T][V]")
+    n, T, V = target.shape
+    _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
+    if draft is not None:
+        _tensor(draft, "tree_verify: draft", (n, T, V), torch.float32, dev)
+    _tensor(tokens, "tree_verify: tokens", (n, T), torch.int32, dev)
+    _tensor(uniforms, "tree_verify: uniforms", (n, T), torch.float32, dev)
+    _tree_tensors("tree_verify", parents, counts, n, T, dev)
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=torch.int32, device=dev) for shape in ((n,), (n, T), (n,)))
+    for t, shape in zip(out, ((n,), (n, T), (n,))):
+        _tensor(t, "tree_verify: out", shape, torch.int32, dev)
+    ws = _space(workspace, lambda _: B.selkv_tree_verify_workspace_size(n, T, V), None, dev, st)
+    accepted, path, next_token = out
+    B.check(B.selkv_tree_verify(n, T, parents, counts, V, tokens, uniforms, target, draft, accepted, path, next_token, ws.buf,
+                                ws.nbytes, st), "selkv_tree_verify")
+    return accepted, path, next_token
+
+
+def tree_commit(caches, K_new, V_new, path: torch.Tensor, accepted: torch.Tensor, workspace: Optional[Workspace] = None,
+                stream=None) -> None:
+    """selkv_tree_commit: the accepted rows of K_new, V_new [B][Hkv][T][d] behind those of a cache, in place; or lists of
+    them: the caches of a model's layers, of one shape."""
+    if isinstance(caches, CompressedCache):
+        caches, K_new, V_new = [caches], [K_new], [V_new]
+    if not caches or len(K_new) != len(caches) or len(V_new) != len(caches):
+        _bad("tree_commit: new rows for each cache")
+    s, dev = caches[0].shape, _cuda(path, "tree_commit: path")
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return tree_commit(caches, K_new, V_new, path, accepted, workspace)
+    st = _raw_stream(dev.index)
+    if path.dim() != 2:
+        _bad("tree_commit: path [B][T]")
+    T, dt = path.shape[1], _TORCH_DTYPE[s.dtype]
+    _tensor(path, "tree_commit: path", (s.batch, T), torch.int32, dev)
+    _tensor(accepted, "tree_commit: accepted", (s.batch,), torch.int32, dev)
+    rows, new = (s.batch, s.num_kv_heads, s.m_cap), (s.batch, s.num_kv_heads, T, s.head_dim)
+    for c, k, v in zip(caches, K_new, V_new):
+        if bytes(c.shape) != bytes(s):
+            _bad("tree_commit: caches of one shape")
+        _tensor(c.K_c, "tree_commit: K_c", rows + (s.head_dim,), dt, dev)
+        _tensor(c.V_c, "tree_commit: V_c", rows + (s.head_dim,), dt, dev)
+        _tensor(c.lengths, "tree_commit: lengths", (s.batch,), torch.int32, dev)
+        if c.bias is not None:
+            _tensor(c.bias, "tree_commit: bias", rows, torch.float32, dev)
+        _tensor(k, "tree_commit: K_new", new, dt, dev)
+        _tensor(v, "tree_commit: V_new", new, dt, dev)
+    ws = _space(workspace, B.selkv_tree_commit_workspace_size, s, dev, st)
+    B.check(B.selkv_tree_commit(s, T, path, accepted, K_new, V_new, [c.K_c for c in caches], [c.V_c for c in caches],
+                                [c.bias for c in caches], [c.lengths for c in caches], ws.buf, ws.nbytes, st),
+            "selkv_tree_commit")

@@ -6,6 +6,7 @@
 
 #include "quant.cuh"
 #include "selkv_internal.cuh"
+#include "tree.cuh"
 
 namespace selkv {
 cudaError_t launch_setup(const CompressArgs& a, const SeqTable& tab, cudaStream_t s);
@@ -195,6 +196,58 @@ selkv_status qcache_of(const selkv_shape& s, const selkv_qcache* c, QCache* q) {
   q->bias = c->bias;
   q->lengths = c->lengths;
   return SELKV_OK;
+}
+
+// Attention of a tree's tokens.  The error word comes first, as everywhere; nothing in the workspace has to be zero.
+struct TreePlan {
+  size_t before, partial, total;
+  int R, block_rows, blocks, ctas, rec_rows;
+};
+
+TreePlan plan_tree(const selkv_shape& s, int tokens) {
+  TreePlan p{};
+  size_t off = sizeof(WsHeader);
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += round256(bytes);
+    return o;
+  };
+  p.R = s.num_q_heads / s.num_kv_heads * tokens;
+  p.block_rows = tree_block_rows(s.dtype, p.R);
+  p.blocks = (p.R + p.block_rows - 1) / p.block_rows;
+  p.rec_rows = p.blocks > 1 ? p.block_rows : (p.R + 3) / 4 * 4;
+  p.ctas = tree_ctas(s.dtype, s.head_dim, p.R);
+  p.before = take((size_t)(s.batch + 2) * 4);
+  p.partial = take((size_t)p.ctas * 2 * tree_record_floats(p.rec_rows, s.head_dim) * 4);
+  p.total = off;
+  return p;
+}
+
+bool tree_rows_ok(const selkv_shape& s) {
+  return (s.head_dim == 64 || s.head_dim == 128) && (int64_t)s.batch * s.num_kv_heads * s.m_cap < (int64_t)1 << 31;
+}
+constexpr int32_t kMaxVocab = 1 << 20;
+bool tree_ok(const selkv_tree* t) {
+  return t != nullptr && t->tokens >= 1 && t->tokens <= SELKV_MAX_TREE && aligned(t->parents, 4) && aligned(t->counts, 4);
+}
+
+constexpr double kTwoPi = 6.283185307179586476925;
+
+// Radians per position of pair f.
+double rope_frequency(int f, int rot, double theta, const selkv_rope_scaling* s) {
+  const double w = std::pow(theta, -2.0 * f / rot);
+  if (s == nullptr || s->kind == SELKV_ROPE_SCALE_NONE) return w;
+  if (s->kind == SELKV_ROPE_SCALE_LINEAR) return w / s->factor;
+  double keep;
+  if (s->kind == SELKV_ROPE_SCALE_WAVELENGTH) {
+    keep = (s->original * w / kTwoPi - s->low) / (s->high - s->low);
+  } else {
+    auto pair_of = [&](double turns) { return rot * std::log(s->original / (kTwoPi * turns)) / (2.0 * std::log(theta)); };
+    const double i0 = std::fmax(0.0, std::floor(pair_of(s->high))), i1 = std::fmin(rot - 1.0, std::ceil(pair_of(s->low)));
+    keep = 1.0 - (f - i0) / std::fmax(i1 - i0, 0.001);
+  }
+  keep = std::fmin(1.0, std::fmax(0.0, keep));
+  return keep * w + (1.0 - keep) * w / s->factor;
 }
 
 template <typename T>
@@ -680,6 +733,206 @@ selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv_qcache* c
   a.partial = at<float>(workspace, plan.partial);
   const cudaError_t e = launch_decode_q(a, reinterpret_cast<cudaStream_t>(stream));
   g_launches += kDecodeKernels;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+selkv_status selkv_rotary_init(selkv_rotary* plan, int32_t rot_dim, int32_t layout, double theta,
+                               const selkv_rope_scaling* scaling) {
+  if (plan == nullptr || rot_dim < 2 || rot_dim > SELKV_ROTARY_MAX_DIM || (rot_dim & 1) != 0) return SELKV_ERR_INVALID_ARG;
+  if (layout != SELKV_ROPE_HALF && layout != SELKV_ROPE_INTERLEAVED) return SELKV_ERR_INVALID_ARG;
+  if (!std::isfinite(theta) || theta <= 0.0) return SELKV_ERR_INVALID_ARG;
+  double amplitude = 1.0;
+  if (scaling != nullptr) {
+    const selkv_rope_scaling& c = *scaling;
+    if (c.kind < SELKV_ROPE_SCALE_NONE || c.kind > SELKV_ROPE_SCALE_RAMP) return SELKV_ERR_INVALID_ARG;
+    if (!std::isfinite(c.amplitude) || c.amplitude < 0.0) return SELKV_ERR_INVALID_ARG;
+    if (c.kind != SELKV_ROPE_SCALE_NONE && !(std::isfinite(c.factor) && c.factor > 0.0)) return SELKV_ERR_INVALID_ARG;
+    if (c.kind == SELKV_ROPE_SCALE_WAVELENGTH || c.kind == SELKV_ROPE_SCALE_RAMP) {
+      if (c.original < 1 || !std::isfinite(c.high) || !(c.low > 0.0 && c.low < c.high)) return SELKV_ERR_INVALID_ARG;
+      if (c.kind == SELKV_ROPE_SCALE_RAMP && theta <= 1.0) return SELKV_ERR_INVALID_ARG;
+    }
+    if (c.amplitude > 0.0) amplitude = c.amplitude;
+    else if (c.kind == SELKV_ROPE_SCALE_RAMP && c.factor > 1.0) amplitude = 0.1 * std::log(c.factor) + 1.0;
+  }
+  uint64_t turns[SELKV_ROTARY_MAX_DIM / 2] = {};
+  for (int f = 0; f < rot_dim / 2; ++f) {
+    const double t = rope_frequency(f, rot_dim, theta, scaling) / kTwoPi;
+    if (!std::isfinite(t)) return SELKV_ERR_INVALID_ARG;
+    turns[f] = (uint64_t)std::ldexp(t - std::floor(t), 64);  // whole turns fall away (below 1: within 64 bits)
+  }
+  plan->layout = layout;
+  plan->rot_dim = rot_dim;
+  plan->amplitude = (float)amplitude;
+  plan->reserved = 0;
+  std::memcpy(plan->turns, turns, sizeof(turns));
+  return SELKV_OK;
+}
+
+selkv_status selkv_rotary_apply(const selkv_shape* shape, const selkv_rotary* plan, int32_t tokens,
+                                const int32_t* positions, const void* q, const void* k, void* q_out, void* k_out,
+                                int32_t transpose, selkv_stream_t stream) {
+  if (!shape_ok(shape) || plan == nullptr) return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  if (s.head_dim != 64 && s.head_dim != 128) return SELKV_ERR_UNSUPPORTED;
+  if ((plan->layout != SELKV_ROPE_HALF && plan->layout != SELKV_ROPE_INTERLEAVED) || plan->rot_dim < 2 ||
+      plan->rot_dim > s.head_dim || (plan->rot_dim & 1) != 0 || !std::isfinite(plan->amplitude))
+    return SELKV_ERR_INVALID_ARG;
+  if (tokens < 1 || positions == nullptr || !aligned(positions, 4)) return SELKV_ERR_INVALID_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (q == nullptr && k == nullptr))
+    return SELKV_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16)) return SELKV_ERR_INVALID_ARG;
+  RotaryArgs a{};
+  a.dtype = s.dtype;
+  a.B = s.batch;
+  a.Hq = s.num_q_heads;
+  a.Hkv = s.num_kv_heads;
+  a.D = s.head_dim;
+  a.T = tokens;
+  a.rot = plan->rot_dim;
+  a.layout = plan->layout;
+  a.amplitude = plan->amplitude;
+  a.sign = transpose != 0 ? -1.f : 1.f;
+  a.positions = positions;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  std::memcpy(a.turns, plan->turns, sizeof(a.turns));
+  const cudaError_t e = launch_rotary(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 1;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+size_t selkv_tree_attn_workspace_size(const selkv_shape* shape, int32_t tokens) {
+  if (!shape_ok(shape) || !tree_rows_ok(*shape) || shape->m_cap < 1 || tokens < 1 || tokens > SELKV_MAX_TREE) return 0;
+  return plan_tree(*shape, tokens).total;
+}
+
+selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tree* tree, const void* q, const void* K_c,
+                             const void* V_c, const float* bias, const int32_t* lengths, const void* k_new,
+                             const void* v_new, void* out, void* workspace, size_t workspace_bytes,
+                             selkv_stream_t stream) {
+  if (!shape_ok(shape) || !tree_ok(tree)) return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  if (s.head_dim != 64 && s.head_dim != 128) return SELKV_ERR_UNSUPPORTED;
+  if (s.m_cap < 1) return SELKV_ERR_INVALID_ARG;
+  const void* tensors[] = {q, K_c, V_c, lengths, k_new, v_new, out};
+  for (const void* t : tensors)
+    if (t == nullptr || !aligned(t, 16)) return SELKV_ERR_INVALID_ARG;
+  if (!aligned(bias, 16)) return SELKV_ERR_INVALID_ARG;
+  if (!tree_rows_ok(s)) return SELKV_ERR_UNSUPPORTED;
+  const TreePlan plan = plan_tree(s, tree->tokens);
+  if (workspace == nullptr || !aligned(workspace, 256)) return SELKV_ERR_WORKSPACE;
+  if (workspace_bytes < plan.total) return SELKV_ERR_WORKSPACE;
+  TreeArgs a{};
+  a.dtype = s.dtype;
+  a.B = s.batch;
+  a.Hq = s.num_q_heads;
+  a.Hkv = s.num_kv_heads;
+  a.G = s.num_q_heads / s.num_kv_heads;
+  a.D = s.head_dim;
+  a.m_cap = s.m_cap;
+  a.T = tree->tokens;
+  a.R = plan.R;
+  a.blocks = plan.blocks;
+  a.rec_rows = plan.rec_rows;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)s.head_dim));
+  a.q = q;
+  a.Kc = K_c;
+  a.Vc = V_c;
+  a.bias = bias;
+  a.lengths = lengths;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.parents = tree->parents;
+  a.counts = tree->counts;
+  a.out = out;
+  a.flags = at<uint32_t>(workspace, 0);
+  a.before = at<int32_t>(workspace, plan.before);
+  a.partial = at<float>(workspace, plan.partial);
+  const cudaError_t e = launch_tree_attn(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 2;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+size_t selkv_tree_verify_workspace_size(int32_t batch, int32_t tokens, int32_t vocab) {
+  if (batch < 1 || batch > SELKV_MAX_BATCH || tokens < 1 || tokens > SELKV_MAX_TREE || vocab < 1 || vocab > kMaxVocab) return 0;
+  return sizeof(WsHeader);
+}
+
+selkv_status selkv_tree_verify(int32_t batch, const selkv_tree* tree, int32_t vocab, const int32_t* tokens,
+                               const float* uniforms, const float* target, const float* draft, int32_t* accepted,
+                               int32_t* path, int32_t* next_token, void* workspace, size_t workspace_bytes,
+                               selkv_stream_t stream) {
+  if (!tree_ok(tree) || batch < 1 || batch > SELKV_MAX_BATCH || vocab < 1 || vocab > kMaxVocab) return SELKV_ERR_INVALID_ARG;
+  const void* small[] = {tokens, uniforms, accepted, path, next_token};
+  for (const void* t : small)
+    if (t == nullptr || !aligned(t, 4)) return SELKV_ERR_INVALID_ARG;
+  if (target == nullptr || !aligned(target, 16) || !aligned(draft, 16)) return SELKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < sizeof(WsHeader)) return SELKV_ERR_WORKSPACE;
+  VerifyArgs a{};
+  a.B = batch;
+  a.T = tree->tokens;
+  a.V = vocab;
+  a.parents = tree->parents;
+  a.counts = tree->counts;
+  a.tokens = tokens;
+  a.uniforms = uniforms;
+  a.target = target;
+  a.draft = draft;
+  a.accepted = accepted;
+  a.path = path;
+  a.next = next_token;
+  a.flags = at<uint32_t>(workspace, 0);
+  const cudaError_t e = launch_tree_verify(a, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 1;
+  return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
+}
+
+size_t selkv_tree_commit_workspace_size(const selkv_shape* shape) {
+  if (!shape_ok(shape)) return 0;
+  return sizeof(WsHeader);
+}
+
+selkv_status selkv_tree_commit(const selkv_shape* shape, int32_t num_layers, int32_t tokens, const int32_t* path,
+                               const int32_t* accepted, const void* const* K_new, const void* const* V_new,
+                               void* const* K_c, void* const* V_c, float* const* bias, int32_t* const* lengths,
+                               void* workspace, size_t workspace_bytes, selkv_stream_t stream) {
+  if (!shape_ok(shape) || K_new == nullptr || V_new == nullptr || K_c == nullptr || V_c == nullptr || lengths == nullptr)
+    return SELKV_ERR_INVALID_ARG;
+  const selkv_shape& s = *shape;
+  if (s.head_dim != 64 && s.head_dim != 128) return SELKV_ERR_UNSUPPORTED;
+  if (num_layers < 1 || num_layers > kMaxLayers || tokens < 1 || tokens > SELKV_MAX_TREE || s.m_cap < 1)
+    return SELKV_ERR_INVALID_ARG;
+  if (path == nullptr || accepted == nullptr || !aligned(path, 4) || !aligned(accepted, 4)) return SELKV_ERR_INVALID_ARG;
+  CommitLayers layers{};
+  for (int l = 0; l < num_layers; ++l) {
+    const void* tensors[] = {K_new[l], V_new[l], K_c[l], V_c[l], lengths[l]};
+    for (const void* t : tensors)
+      if (t == nullptr || !aligned(t, 16)) return SELKV_ERR_INVALID_ARG;
+    if (bias != nullptr && !aligned(bias[l], 16)) return SELKV_ERR_INVALID_ARG;
+    layers.k_new[l] = K_new[l];
+    layers.v_new[l] = V_new[l];
+    layers.K[l] = K_c[l];
+    layers.V[l] = V_c[l];
+    layers.bias[l] = bias != nullptr ? bias[l] : nullptr;
+    layers.lengths[l] = lengths[l];
+    for (int k = 0; k < l; ++k)
+      if (lengths[k] == lengths[l] || K_c[k] == K_c[l] || V_c[k] == V_c[l]) return SELKV_ERR_INVALID_ARG;
+  }
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < sizeof(WsHeader)) return SELKV_ERR_WORKSPACE;
+  CommitArgs a{};
+  a.B = s.batch;
+  a.Hkv = s.num_kv_heads;
+  a.T = tokens;
+  a.m_cap = s.m_cap;
+  a.layers = num_layers;
+  a.row_bytes = s.head_dim * (s.dtype == SELKV_BF16 ? 2 : 4);
+  a.path = path;
+  a.accepted = accepted;
+  a.flags = at<uint32_t>(workspace, 0);
+  const cudaError_t e = launch_tree_commit(a, layers, reinterpret_cast<cudaStream_t>(stream));
+  g_launches += 2;
   return e == cudaSuccess ? SELKV_OK : cuda_fail(e);
 }
 

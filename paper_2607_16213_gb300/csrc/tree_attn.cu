@@ -1,0 +1,304 @@
+// Compensated attention of a tree of drafted tokens (selkv_tree_attn): fp32 on CUDA cores, and for both
+// types the kernel that joins the pieces of a unit.
+//
+//   out[t] = sum_i p_i v_i,  p = softmax(q_t . k_i / sqrt(d) + bias_i) over the cached rows, token t's ancestors and t.
+//
+// The G T query rows of a KV head meet its rows together: the cache is read once per block of rows.  The list
+// of all (sequence, KV head, row block, key tile) is cut into equal shares of consecutive tiles, one a CTA, so
+// ragged lengths leave no CTA idle; a unit that lies in one share is finished there, the others'
+// pieces go through memory as (reference, sum, output) and are joined in list order by tree_join_kernel: results
+// do not depend on scheduling.
+#include <cfloat>
+
+#include "tree.cuh"
+
+namespace selkv {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Finish row `row` of a unit: elements d .. d + 3.
+template <typename T>
+__device__ __forceinline__ void put_out(const TreeArgs& a, int b, int kv, int r, int d, const float (&x)[4]) {
+  store4(static_cast<T*>(a.out) + (((size_t)b * a.Hq + kv * a.G) * a.T + r) * a.D + d, x);
+}
+
+// fp32: tiles of 64 keys, a thread holds RPT rows x 4 keys of the logits and RPT rows x D / 16 elements of the
+// output; 16 threads share a row, so its statistics and probabilities stay within half a warp.
+// The products run on the FMA units: R rows cost 4 R d operations per key for 8 d bytes, so above about 20 rows
+// a KV head the arithmetic bounds it, below the loads.
+template <typename T, int D, int RPT>
+__global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
+  constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;
+  constexpr int LD = D + 4, PLD = KEYS + 4;  // (padded: 16 rows' float4 in different banks)
+  constexpr int NE = D / 64;                 // float4 of the output per thread and row
+  extern __shared__ __align__(16) float sm[];
+  float* Qs = sm;                 // [RT][LD]
+  float* Ks = Qs + RT * LD;       // [KEYS][LD]; the probabilities [RT][PLD] lie over it once it is read
+  float* Vs = Ks + KEYS * LD;     // [KEYS][D]
+  float* bs = Vs + KEYS * D;      // [KEYS] bias in base 2, -inf: the key is out
+  uint4* seen = reinterpret_cast<uint4*>(bs + KEYS);                       // [SELKV_MAX_TREE]
+  int32_t* before = reinterpret_cast<int32_t*>(seen + SELKV_MAX_TREE);     // [B + 1]
+  __shared__ int8_t up[SELKV_MAX_TREE];
+  float* Ps = Ks;
+  static_assert(RT * PLD <= KEYS * LD, "probabilities fit the keys' place");
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+
+  tree_list<KEYS>(a, before, blockIdx.x == 0);
+  const int total = before[a.B], share = tree_share(total, gridDim.x);
+  if (blockIdx.x == 0) {
+    for (int b = tid; b <= a.B; b += kThreads) a.before[b] = before[b];
+    if (tid == 0) a.before[a.B + 1] = share;
+  }
+  int pos = (int)min((long long)total, (long long)blockIdx.x * share);
+  const int end = min(total, pos + share);
+  while (pos < end) {
+    const TreePiece p = tree_piece<KEYS>(a, before, pos, end);
+    pos += p.count;
+    const size_t bk = (size_t)p.b * a.Hkv + p.kv;
+    const int cache_tiles = (p.L + KEYS - 1) / KEYS;
+    const int row0 = p.blk * RT, rows = min(RT, a.R - row0);
+    __syncthreads();  // the last piece's rows are read
+    const T* q = static_cast<const T*>(a.q) + (((size_t)p.b * a.Hq + p.kv * a.G) * a.T + row0) * D;
+    for (int i = tid; i < RT * (D / 4); i += kThreads) {
+      const int r = i / (D / 4), d = i % (D / 4) * 4;
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < rows) load4(q + (size_t)r * D + d, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= a.scale_log2;
+      store4(Qs + r * LD + d, x);
+    }
+    if (p.first + p.count > cache_tiles) tree_ancestors<kThreads>(a, p.b, p.n, seen, up, tid, 1);
+    float m[RPT], l[RPT], o[RPT][NE * 4];
+    int tok[RPT];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      tok[i] = (row0 + ty * RPT + i) % a.T;
+#pragma unroll
+      for (int e = 0; e < NE * 4; ++e) o[i][e] = 0.f;
+    }
+    for (int t = p.first; t < p.first + p.count; ++t) {
+      const bool drafts = t >= cache_tiles;
+      const int key0 = (drafts ? t - cache_tiles : t) * KEYS, keys = min(KEYS, (drafts ? p.n : p.L) - key0);
+      const T* kp = static_cast<const T*>(drafts ? a.k_new : a.Kc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
+      const T* vp = static_cast<const T*>(drafts ? a.v_new : a.Vc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
+      const float* bias = drafts || a.bias == nullptr ? nullptr : a.bias + bk * a.m_cap + key0;
+      __syncthreads();  // the last tile is read (and Q is there)
+      for (int i = tid; i < KEYS * (D / 4); i += kThreads) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+        // (a row without weight may hold anything)
+        if (r < keys && (bias == nullptr || bias[r] != -INFINITY)) {
+          load4(kp + (size_t)r * D + d, x);
+          load4(vp + (size_t)r * D + d, y);
+        }
+        store4(Ks + r * LD + d, x);
+        store4(Vs + r * D + d, y);
+      }
+      if (tid < KEYS) bs[tid] = tid >= keys ? -INFINITY : bias != nullptr ? bias[tid] * kLog2e : 0.f;
+      __syncthreads();
+      // logits of rows ty RPT + i and keys tx + 16 j
+      float s[RPT][4];
+#pragma unroll
+      for (int i = 0; i < RPT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        float kx[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load4(Ks + (tx + 16 * j) * LD + d, kx[j]);
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          float qx[4];
+          load4(Qs + (ty * RPT + i) * LD + d, qx);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][j] = fmaf(qx[e], kx[j][e], s[i][j]);
+        }
+      }
+      __syncthreads();  // the keys are read: the probabilities go there
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        float mx = -INFINITY;
+        bool nan = false;
+        const uint4 sees = drafts ? seen[tok[i]] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = tx + 16 * j;
+          const float b = bs[key];
+          bool in = b != -INFINITY;
+          if (drafts) {
+            const uint32_t w = key0 == 0 ? (key < 32 ? sees.x : sees.y) : (key < 32 ? sees.z : sees.w);
+            in = in && ((w >> (key & 31)) & 1u);
+          }
+          s[i][j] = in ? s[i][j] + b : -INFINITY;
+          nan = nan || s[i][j] != s[i][j];
+          mx = fmaxf(mx, s[i][j]);
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+        const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2f(m[i] - ref);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = exp2f(s[i][j] - ref);
+          Ps[(ty * RPT + i) * PLD + tx + 16 * j] = x;
+          sum += x;
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        m[i] = mn;
+        l[i] = l[i] * f + sum;
+#pragma unroll
+        for (int e = 0; e < NE * 4; ++e) o[i][e] *= f;
+      }
+      __syncwarp();  // a row's probabilities are written and read by the same half warp
+#pragma unroll 2
+      for (int k = 0; k < KEYS; k += 4) {
+        float px[RPT][4];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) load4(Ps + (ty * RPT + i) * PLD + k, px[i]);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          float v[NE * 4];
+#pragma unroll
+          for (int e = 0; e < NE; ++e) load4(Vs + (k + kk) * D + tx * 4 + 64 * e, reinterpret_cast<float(&)[4]>(v[e * 4]));
+#pragma unroll
+          for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int e = 0; e < NE * 4; ++e) {
+              // (an unseen token's row may hold infinities or NaN)
+              const float x = drafts && px[i][kk] == 0.f ? 0.f : v[e];
+              o[i][e] = fmaf(px[i][kk], x, o[i][e]);
+            }
+        }
+      }
+    }
+    if (p.whole()) {
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const int r = ty * RPT + i;
+        if (r < rows && tok[i] < p.n) {
+          const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            const float x[4] = {o[i][e * 4] * inv, o[i][e * 4 + 1] * inv, o[i][e * 4 + 2] * inv, o[i][e * 4 + 3] * inv};
+            put_out<T>(a, p.b, p.kv, row0 + r, tx * 4 + 64 * e, x);
+          }
+        }
+      }
+    } else {
+      float* rec = tree_record(a, blockIdx.x, p);
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const int r = ty * RPT + i;
+        if (r < rows) {
+#pragma unroll
+          for (int e = 0; e < NE; ++e) {
+            const float x[4] = {o[i][e * 4], o[i][e * 4 + 1], o[i][e * 4 + 2], o[i][e * 4 + 3]};
+            store4(rec + ((size_t)(tx + 16 * e) * a.rec_rows + r) * 4, x);
+          }
+          if (tx == 0) reinterpret_cast<float2*>(rec + (size_t)a.rec_rows * D)[r] = make_float2(m[i], l[i]);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int D, int RPT>
+cudaError_t launch_simt(const TreeArgs& a, int ctas, cudaStream_t s) {
+  constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;
+  const int smem = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16 + (a.B + 1) * 4;
+  constexpr int most = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16 + (SELKV_MAX_BATCH + 1) * 4;
+  if (const cudaError_t e = set_smem_once<tree_simt_kernel<T, D, RPT>>(most); e != cudaSuccess) return e;
+  tree_simt_kernel<T, D, RPT><<<ctas, kThreads, smem, s>>>(a);
+  return cudaGetLastError();
+}
+
+// ---- joining the pieces of a unit ----------------------------------------------------------
+// Eight rows of a unit a CTA; a thread four elements of one.  Units that one CTA finished have nothing to join.
+constexpr int kJoinRows = 8;
+template <typename T, int D>
+__global__ __launch_bounds__(kJoinRows * D / 4) void tree_join_kernel(TreeArgs a, int unit_rows) {
+  pdl_wait();
+  const int per = (unit_rows + kJoinRows - 1) / kJoinRows;
+  const int blk = blockIdx.x / per, r = (blockIdx.x - blk * per) * kJoinRows + threadIdx.x % kJoinRows;
+  const int d4 = threadIdx.x / kJoinRows, kv = blockIdx.y, b = blockIdx.z;
+  const int lo = a.before[b], tiles = (a.before[b + 1] - lo) / (a.Hkv * a.blocks), share = a.before[a.B + 1];
+  if (tiles == 0) return;
+  const int u0 = lo + (kv * a.blocks + blk) * tiles, u1 = u0 + tiles;
+  const int c0 = u0 / share, c1 = (u1 - 1) / share;
+  const int row = blk * unit_rows + r;
+  int n = a.counts != nullptr ? a.counts[b] : a.T;
+  n = min(n, a.T);
+  if (c0 == c1 || r >= unit_rows || row >= a.R || row % a.T >= n) return;
+  const size_t rec = tree_record_floats(a.rec_rows, D);
+  // the first piece lies in its CTA's second record, the others in their CTAs' first
+  auto record = [&](int c) { return a.partial + (size_t)(c * 2 + (c == c0 ? 1 : 0)) * rec; };
+  // (the unit's first tile may be its CTA's first: the record is the second all the same)
+  float M = -INFINITY;
+#pragma unroll 8
+  for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(record(c) + (size_t)a.rec_rows * D) + r).x);
+  const float ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int c = c0; c <= c1; ++c) {
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(record(c) + (size_t)a.rec_rows * D) + r);
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(record(c)) + (size_t)d4 * a.rec_rows + r);
+    const float w = exp2f(ml.x - ref);
+    L = fmaf(ml.y, w, L);
+    // (a piece without weight has outputs 0)
+    x[0] = fmaf(v.x, w, x[0]);
+    x[1] = fmaf(v.y, w, x[1]);
+    x[2] = fmaf(v.z, w, x[2]);
+    x[3] = fmaf(v.w, w, x[3]);
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
+  put_out<T>(a, b, kv, row, d4 * 4, x);
+}
+
+template <typename T, int D>
+cudaError_t launch_join(const TreeArgs& a, cudaStream_t s) {
+  const int unit_rows = tree_block_rows(a.dtype, a.R);
+  const int used = a.blocks > 1 ? unit_rows : a.R;
+  const dim3 grid((unsigned)(((used + kJoinRows - 1) / kJoinRows) * a.blocks), (unsigned)a.Hkv, (unsigned)a.B);
+  return launch_chained(true, tree_join_kernel<T, D>, grid, dim3(kJoinRows * D / 4), 0, s, a, used);
+}
+
+}  // namespace
+
+int tree_ctas(int dtype, int D, int R) {
+  (void)dtype;
+  (void)D;
+  (void)R;
+  return 2 * kPlanSMs;
+}
+
+cudaError_t launch_tree_attn(const TreeArgs& a, cudaStream_t s) {
+  const int ctas = tree_ctas(a.dtype, a.D, a.R);
+  cudaError_t e;
+  if (a.dtype == SELKV_BF16) {
+    if (a.R <= 16)
+      e = a.D == 128 ? launch_simt<__nv_bfloat16, 128, 1>(a, ctas, s) : launch_simt<__nv_bfloat16, 64, 1>(a, ctas, s);
+    else
+      e = a.D == 128 ? launch_simt<__nv_bfloat16, 128, 4>(a, ctas, s) : launch_simt<__nv_bfloat16, 64, 4>(a, ctas, s);
+    if (e != cudaSuccess) return e;
+    return a.D == 128 ? launch_join<__nv_bfloat16, 128>(a, s) : launch_join<__nv_bfloat16, 64>(a, s);
+  }
+  if (a.R <= 16)
+    e = a.D == 128 ? launch_simt<float, 128, 1>(a, ctas, s) : launch_simt<float, 64, 1>(a, ctas, s);
+  else
+    e = a.D == 128 ? launch_simt<float, 128, 4>(a, ctas, s) : launch_simt<float, 64, 4>(a, ctas, s);
+  if (e != cudaSuccess) return e;
+  return a.D == 128 ? launch_join<float, 128>(a, s) : launch_join<float, 64>(a, s);
+}
+
+}  // namespace selkv
