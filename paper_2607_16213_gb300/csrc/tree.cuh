@@ -146,13 +146,14 @@ __device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, 
 }
 
 constexpr int kTreeTcKeys = 128, kTreeSimtKeys = 64;  // keys of a tile
-// Rows of a block.
+// Rows of a block (tensor cores: two accumulators of 128 rows where one does not hold them).
 inline int tree_block_rows(int dtype, int R) {
-  (void)dtype;
+  if (dtype == SELKV_BF16) return R <= 128 ? 128 : 256;
   return R <= 16 ? 16 : 64;
 }
 int tree_ctas(int dtype, int D, int R);  // CTAs of a launch
 cudaError_t launch_tree_attn(const TreeArgs& a, cudaStream_t s);
+cudaError_t launch_tree_tc(const TreeArgs& a, int ctas, cudaStream_t s);
 
 // ---- the other steps ----------------------------------------------------------------------
 struct RotaryArgs {

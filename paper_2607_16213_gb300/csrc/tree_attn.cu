@@ -276,20 +276,16 @@ cudaError_t launch_join(const TreeArgs& a, cudaStream_t s) {
 }  // namespace
 
 int tree_ctas(int dtype, int D, int R) {
-  (void)dtype;
   (void)D;
   (void)R;
-  return 2 * kPlanSMs;
+  return dtype == SELKV_BF16 ? kPlanSMs : 2 * kPlanSMs;
 }
 
 cudaError_t launch_tree_attn(const TreeArgs& a, cudaStream_t s) {
   const int ctas = tree_ctas(a.dtype, a.D, a.R);
   cudaError_t e;
   if (a.dtype == SELKV_BF16) {
-    if (a.R <= 16)
-      e = a.D == 128 ? launch_simt<__nv_bfloat16, 128, 1>(a, ctas, s) : launch_simt<__nv_bfloat16, 64, 1>(a, ctas, s);
-    else
-      e = a.D == 128 ? launch_simt<__nv_bfloat16, 128, 4>(a, ctas, s) : launch_simt<__nv_bfloat16, 64, 4>(a, ctas, s);
+    e = launch_tree_tc(a, ctas, s);
     if (e != cudaSuccess) return e;
     return a.D == 128 ? launch_join<__nv_bfloat16, 128>(a, s) : launch_join<__nv_bfloat16, 64>(a, s);
   }
