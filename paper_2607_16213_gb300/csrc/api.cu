@@ -217,7 +217,7 @@ TreePlan plan_tree(const selkv_shape& s, int tokens) {
   p.blocks = (p.R + p.block_rows - 1) / p.block_rows;
   p.rec_rows = p.blocks > 1 ? p.block_rows : (p.R + 3) / 4 * 4;
   p.ctas = tree_ctas(s.dtype, s.head_dim, p.R);
-  p.before = take((size_t)(s.batch + 2) * 4);
+  p.before = take((size_t)(s.batch + 3) * 4);
   p.partial = take((size_t)p.ctas * 2 * tree_record_floats(p.rec_rows, s.head_dim) * 4);
   p.total = off;
   return p;

@@ -26,8 +26,8 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 
 }  // namespace
 
-// Encodings are cached by (base, rows, d, box rows): the same buffers come back call after call
-// (a decode step per layer), and a map depends on nothing else.
+// Encodings are kept by (base, rows, d, box rows): the same buffers come back call after call (a decode step per
+// layer), and a map depends on nothing else.  A place per hash, taken by the last one that asked.
 namespace {
 struct MapEntry {
   const void* base;
@@ -35,21 +35,25 @@ struct MapEntry {
   int d, box;
   CUtensorMap map;
 };
-constexpr int kMapCache = 128;
+constexpr int kMapCache = 2048;
 std::mutex g_map_mu;
 MapEntry g_maps[kMapCache];
-int g_map_used = 0, g_map_next = 0;
+
+MapEntry& place_of(const void* base, uint64_t rows, int d, int box_rows) {
+  uint64_t h = reinterpret_cast<uintptr_t>(base) >> 4;
+  h = (h ^ rows * 31u ^ (uint64_t)(d * 257 + box_rows) * 7919u) * 0x9E3779B97F4A7C15ull;
+  return g_maps[h >> 53];
+}
+static_assert(kMapCache == 1 << 11, "the hash's upper 11 bits");
 }  // namespace
 
 bool encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, int box_rows) {
+  MapEntry& e = place_of(base, rows, d, box_rows);
   {
     std::lock_guard<std::mutex> lock(g_map_mu);
-    for (int i = 0; i < g_map_used; ++i) {
-      const MapEntry& e = g_maps[i];
-      if (e.base == base && e.rows == rows && e.d == d && e.box == box_rows) {
-        *map = e.map;
-        return true;
-      }
+    if (base != nullptr && e.base == base && e.rows == rows && e.d == d && e.box == box_rows) {
+      *map = e.map;
+      return true;
     }
   }
   auto fn = encode_fn();
@@ -63,14 +67,11 @@ bool encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, 
          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
   std::lock_guard<std::mutex> lock(g_map_mu);
-  MapEntry& e = g_maps[g_map_next];
   e.base = base;
   e.rows = rows;
   e.d = d;
   e.box = box_rows;
   e.map = *map;
-  g_map_next = (g_map_next + 1) % kMapCache;
-  if (g_map_used < kMapCache) ++g_map_used;
   return true;
 }
 

@@ -24,7 +24,7 @@ struct TreeArgs {
   const int32_t* counts;
   void* out;
   uint32_t* flags;
-  int32_t* before;  // [B + 1] key tiles of the sequences before b, and of all; then tiles a CTA takes
+  int32_t* before;  // [B + 3] the list (TreeList::before and head)
   float* partial;   // [CTA][2] records of tree_record_floats
 };
 
@@ -32,87 +32,171 @@ struct TreeArgs {
 // sum) [rows].  Rows side by side: the lanes of a warp hold a row each.
 __host__ __device__ constexpr size_t tree_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
-// Fewest tiles a CTA takes of a call (below it a partial's way through memory costs more than the tiles).
+// Fewest tiles of a piece where a unit is cut (below it a partial's way through memory costs more than the tiles).
 constexpr int kTreeMinTiles = 2;
+// What ending one piece and beginning another costs a CTA, in tiles.
+constexpr int kTreePieceTiles = 6;
 
-// What a sequence has: cached rows, tokens, and its key tiles (the tokens' own rows are one more), 0 without tokens.
-struct TreeSeq {
-  int L, n, tiles;
+// The work is the list of all units (sequence, KV head, row block) and their key tiles: those of the cached rows,
+// then those of the tokens' own.  Each CTA finds its part from the lengths, in one of two ways.
+//   Equal shares: the tiles of all units in a row, `share` consecutive ones a CTA, so that ragged lengths leave
+//   none idle; a CTA may end one unit and begin another.
+//   A piece a CTA: a unit of t tiles is cut into ceil(t / share) even pieces, with the smallest share that leaves no more
+//   pieces than CTAs.  Taken where there are no more units than CTAs and that share is at most kTreePieceTiles more, what a
+//   second piece costs (one sequence of 25000 rows, 8 KV heads, 152 CTAs: a CTA with two pieces took 36 us, the others 25).
+// In shared memory: the sequences' (cached rows, tokens), and the pieces or tiles of the sequences before each.
+struct TreeList {
+  int32_t* before;  // [B + 1]
+  int2* seq;        // [B]
+  int32_t* head;    // [2] share, 1: a piece a CTA
 };
-template <int KEYS>
-__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int b, bool tell) {
-  int L = a.lengths[b], n = a.counts != nullptr ? a.counts[b] : a.T;
-  if (L < 0 || L > a.m_cap || n < 0 || n > a.T) {
-    if (tell) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
-    L = min(max(L, 0), a.m_cap);
-    n = min(max(n, 0), a.T);
-  }
-  return {L, n, n > 0 ? (L + KEYS - 1) / KEYS + (n + KEYS - 1) / KEYS : 0};
+__host__ __device__ constexpr int tree_list_bytes(int B) { return (B + 1) * 12 + 12; }  // (before lies behind seq)
+__device__ __forceinline__ TreeList tree_list_at(void* smem, int B) {  // 8-byte aligned
+  int2* seq = static_cast<int2*>(smem);
+  int32_t* before = reinterpret_cast<int32_t*>(seq + B);
+  return {before, seq, before + B + 1};
 }
-
-// The list of all (sequence, KV head, row block, key tile) in that order is cut into equal shares, one a
-// CTA.  `before` [B + 1] in shared memory: entries of the list before each sequence.  All threads come here.
 template <int KEYS>
-__device__ __forceinline__ void tree_list(const TreeArgs& a, int32_t* before, bool tell) {
-  for (int b = threadIdx.x; b < a.B; b += blockDim.x) before[b + 1] = tree_seq<KEYS>(a, b, tell).tiles * a.Hkv * a.blocks;
-  if (threadIdx.x == 0) before[0] = 0;
+__device__ __forceinline__ int tree_tiles(int2 seq) {
+  return seq.y > 0 ? (seq.x + KEYS - 1) / KEYS + (seq.y + KEYS - 1) / KEYS : 0;
+}
+// A warp's running sum of `before`'s entries 1 .. B, in place.
+__device__ __forceinline__ void tree_prefix(int32_t* before, int B) {
+  const int lane = threadIdx.x & 31;
+  int sum = 0;
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    int x = b < B ? before[b + 1] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (b < B) before[b + 1] = sum + x;
+    sum += __shfl_sync(0xffffffffu, x, 31);
+  }
+}
+// All threads of the CTA come here; `tell`: this CTA reports lengths and counts out of range.
+template <int KEYS>
+__device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, int ctas, bool tell) {
+  const int per = a.Hkv * a.blocks;  // units of a sequence
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    int L = a.lengths[b], n = a.counts != nullptr ? a.counts[b] : a.T;
+    if (L < 0 || L > a.m_cap || n < 0 || n > a.T) {
+      if (tell) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
+      L = min(max(L, 0), a.m_cap);
+      n = min(max(n, 0), a.T);
+    }
+    w.seq[b] = make_int2(L, n);
+    w.before[b + 1] = tree_tiles<KEYS>(make_int2(L, n)) * per;
+  }
   __syncthreads();
   if (threadIdx.x < 32) {
-    int sum = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-      const int b = b0 + threadIdx.x;
-      int x = b < a.B ? before[b + 1] : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if ((int)threadIdx.x >= o) x += y;
-      }
-      if (b < a.B) before[b + 1] = sum + x;
-      sum += __shfl_sync(0xffffffffu, x, 31);
+    const int lane = threadIdx.x;
+    int units = 0, total = 0;
+    for (int b = lane; b < a.B; b += 32) {
+      const int t = w.before[b + 1];
+      units += t > 0 ? per : 0;
+      total += t;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      units += __shfl_xor_sync(0xffffffffu, units, o);
+      total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
+    int share = max(kTreeMinTiles, (total + ctas - 1) / ctas);
+    bool piece = false;
+    if (units <= ctas) {
+      // (a candidate a lane)
+      const int mine = share + min(lane, kTreePieceTiles);
+      int pieces = 0;
+      for (int b = 0; b < a.B; ++b) pieces += (tree_tiles<KEYS>(w.seq[b]) + mine - 1) / mine * per;
+      const uint32_t fits = __ballot_sync(0xffffffffu, pieces <= ctas);
+      if (fits != 0) {
+        piece = true;
+        share += __ffs(fits) - 1;
+        for (int b = lane; b < a.B; b += 32) w.before[b + 1] = (tree_tiles<KEYS>(w.seq[b]) + share - 1) / share * per;
+      }
+    }
+    if (lane == 0) {
+      w.before[0] = 0;
+      w.head[0] = share;
+      w.head[1] = piece;
+    }
+    __syncwarp();
+    tree_prefix(w.before, a.B);
   }
   __syncthreads();
 }
-__device__ __forceinline__ int tree_share(int total, int ctas) { return max(kTreeMinTiles, (total + ctas - 1) / ctas); }
+// The list for the kernel that joins (by one CTA).
+__device__ __forceinline__ void tree_list_store(const TreeArgs& a, const TreeList& w) {
+  for (int b = threadIdx.x; b < a.B + 3; b += blockDim.x) a.before[b] = w.before[b];  // (head lies behind)
+}
 
-// One piece of a CTA's share: tiles of one (sequence, KV head, row block).
+// The CTA's part: places pos .. end - 1 of the list.
+struct TreeRange {
+  int pos, end;
+};
+__device__ __forceinline__ TreeRange tree_range(const TreeArgs& a, const TreeList& w, int cta) {
+  const int total = w.before[a.B];
+  if (w.head[1]) return {min(cta, total), min(cta + 1, total)};
+  const int p = (int)min((long long)total, (long long)cta * w.head[0]);
+  return {p, min(total, p + w.head[0])};
+}
+// One piece: tiles first .. first + count - 1 of a unit.
 struct TreePiece {
   int b, kv, blk;
   int L, n;      // cached rows, tokens
   int tiles;     // key tiles of the unit
   int first, count;
+  int places;    // of the list
   __device__ __forceinline__ bool whole() const { return count == tiles; }
 };
+// (Not inlined: every role of a CTA asks, and a launch begins with fetching its code, at about a byte a cycle.)
 template <int KEYS>
-__device__ __forceinline__ TreePiece tree_piece(const TreeArgs& a, const int32_t* before, int pos, int end) {
+__device__ __noinline__ TreePiece tree_piece(const TreeArgs& a, const TreeList& w, TreeRange r) {
   int lo = 0, hi = a.B;  // before[lo] <= pos < before[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (before[mid] <= pos) lo = mid;
+    if (w.before[mid] <= r.pos) lo = mid;
     else hi = mid;
   }
-  const TreeSeq s = tree_seq<KEYS>(a, lo, false);
-  const int at = pos - before[lo], unit = at / s.tiles;
+  const int2 s = w.seq[lo];
   TreePiece p;
+  p.tiles = tree_tiles<KEYS>(s);
+  const int at = r.pos - w.before[lo];
+  int unit;
+  if (w.head[1]) {
+    const int pieces = (p.tiles + w.head[0] - 1) / w.head[0];
+    unit = at / pieces;
+    const int j = at - unit * pieces, each = p.tiles / pieces, more = p.tiles - each * pieces;  // `more` pieces have one more
+    p.first = j * each + min(j, more);
+    p.count = each + (j < more ? 1 : 0);
+    p.places = 1;
+  } else {
+    unit = at / p.tiles;
+    p.first = at - unit * p.tiles;
+    p.count = min(p.tiles - p.first, r.end - r.pos);
+    p.places = p.count;
+  }
   p.b = lo;
   p.kv = unit / a.blocks;
   p.blk = unit - p.kv * a.blocks;
-  p.L = s.L;
-  p.n = s.n;
-  p.tiles = s.tiles;
-  p.first = at - unit * s.tiles;
-  p.count = min(s.tiles - p.first, end - pos);
+  p.L = s.x;
+  p.n = s.y;
   return p;
 }
 __device__ __forceinline__ float* tree_record(const TreeArgs& a, int cta, const TreePiece& p) {
   return a.partial + (size_t)(cta * 2 + (p.first > 0 ? 0 : 1)) * tree_record_floats(a.rec_rows, a.D);
 }
 
-// Ancestors of each token of sequence b and the token itself, as bits, into `seen`; by paths of doubling length.
-// Called by threads 0 .. kN - 1 of a barrier `bar` over them (kN >= SELKV_MAX_TREE).
-template <int kN>
-__device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, uint4* seen, int8_t* up, int i, int bar) {
-  if (i < SELKV_MAX_TREE) {
+// The warp's: ancestors of each token of sequence b and the token itself, as bits, into `seen`, by paths of doubling length.
+__device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, uint4* seen, int8_t* up) {
+  constexpr int kPer = SELKV_MAX_TREE / 32;
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int i = lane + 32 * k;
     int p = -1;
     if (i < n) {
       p = a.parents != nullptr ? a.parents[(size_t)b * a.T + i] : i - 1;
@@ -122,30 +206,35 @@ __device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, 
       }
     }
     up[i] = (int8_t)p;
-    const uint32_t bit = 1u << (i & 31);
-    seen[i] = make_uint4(i < 32 ? bit : 0u, (i >> 5) == 1 ? bit : 0u, (i >> 5) == 2 ? bit : 0u, (i >> 5) == 3 ? bit : 0u);
+    const uint32_t bit = 1u << lane;
+    seen[i] = make_uint4(k == 0 ? bit : 0u, k == 1 ? bit : 0u, k == 2 ? bit : 0u, k == 3 ? bit : 0u);
   }
-  named_bar_sync(bar, kN);
+  __syncwarp();
   for (int reach = 1; reach < n; reach <<= 1) {
-    int p = -1, far = -1;
-    uint4 s = make_uint4(0u, 0u, 0u, 0u);
-    if (i < n) {
-      p = up[i];
+    int far[kPer];
+    uint4 s[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = lane + 32 * k, p = i < n ? up[i] : -1;
+      s[k] = seen[i];
+      far[k] = -1;
       if (p >= 0) {
-        s = seen[p];
-        far = up[p];
+        const uint4 t = seen[p];
+        s[k] = make_uint4(s[k].x | t.x, s[k].y | t.y, s[k].z | t.z, s[k].w | t.w);
+        far[k] = up[p];
       }
     }
-    named_bar_sync(bar, kN);
-    if (p >= 0) {
-      seen[i] = make_uint4(seen[i].x | s.x, seen[i].y | s.y, seen[i].z | s.z, seen[i].w | s.w);
-      up[i] = (int8_t)far;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      seen[lane + 32 * k] = s[k];
+      up[lane + 32 * k] = (int8_t)far[k];
     }
-    named_bar_sync(bar, kN);
+    __syncwarp();
   }
 }
 
-constexpr int kTreeTcKeys = 128, kTreeSimtKeys = 64;  // keys of a tile
+constexpr int kTreeTcKeys = 64, kTreeSimtKeys = 64;  // keys of a tile
 // Rows of a block (tensor cores: two accumulators of 128 rows where one does not hold them).
 inline int tree_block_rows(int dtype, int R) {
   if (dtype == SELKV_BF16) return R <= 128 ? 128 : 256;

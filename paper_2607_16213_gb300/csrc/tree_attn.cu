@@ -37,24 +37,20 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
   float* Ks = Qs + RT * LD;       // [KEYS][LD]; the probabilities [RT][PLD] lie over it once it is read
   float* Vs = Ks + KEYS * LD;     // [KEYS][D]
   float* bs = Vs + KEYS * D;      // [KEYS] bias in base 2, -inf: the key is out
-  uint4* seen = reinterpret_cast<uint4*>(bs + KEYS);                       // [SELKV_MAX_TREE]
-  int32_t* before = reinterpret_cast<int32_t*>(seen + SELKV_MAX_TREE);     // [B + 1]
+  uint4* seen = reinterpret_cast<uint4*>(bs + KEYS);  // [SELKV_MAX_TREE]
+  const TreeList list = tree_list_at(seen + SELKV_MAX_TREE, a.B);
   __shared__ int8_t up[SELKV_MAX_TREE];
   float* Ps = Ks;
   static_assert(RT * PLD <= KEYS * LD, "probabilities fit the keys' place");
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
 
-  tree_list<KEYS>(a, before, blockIdx.x == 0);
-  const int total = before[a.B], share = tree_share(total, gridDim.x);
-  if (blockIdx.x == 0) {
-    for (int b = tid; b <= a.B; b += kThreads) a.before[b] = before[b];
-    if (tid == 0) a.before[a.B + 1] = share;
-  }
-  int pos = (int)min((long long)total, (long long)blockIdx.x * share);
-  const int end = min(total, pos + share);
-  while (pos < end) {
-    const TreePiece p = tree_piece<KEYS>(a, before, pos, end);
-    pos += p.count;
+  chain_begin();
+  tree_list<KEYS>(a, list, gridDim.x, blockIdx.x == 0);
+  if (blockIdx.x == 0) tree_list_store(a, list);
+  TreeRange range = tree_range(a, list, blockIdx.x);
+  while (range.pos < range.end) {
+    const TreePiece p = tree_piece<KEYS>(a, list, range);
+    range.pos += p.places;
     const size_t bk = (size_t)p.b * a.Hkv + p.kv;
     const int cache_tiles = (p.L + KEYS - 1) / KEYS;
     const int row0 = p.blk * RT, rows = min(RT, a.R - row0);
@@ -68,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
       for (int e = 0; e < 4; ++e) x[e] *= a.scale_log2;
       store4(Qs + r * LD + d, x);
     }
-    if (p.first + p.count > cache_tiles) tree_ancestors<kThreads>(a, p.b, p.n, seen, up, tid, 1);
+    if (p.first + p.count > cache_tiles && tid < 32) tree_ancestors(a, p.b, p.n, seen, up);  // (the tile loop's barrier is behind it)
     float m[RPT], l[RPT], o[RPT][NE * 4];
     int tok[RPT];
 #pragma unroll
@@ -213,52 +209,66 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
 template <typename T, int D, int RPT>
 cudaError_t launch_simt(const TreeArgs& a, int ctas, cudaStream_t s) {
   constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;
-  const int smem = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16 + (a.B + 1) * 4;
-  constexpr int most = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16 + (SELKV_MAX_BATCH + 1) * 4;
-  if (const cudaError_t e = set_smem_once<tree_simt_kernel<T, D, RPT>>(most); e != cudaSuccess) return e;
-  tree_simt_kernel<T, D, RPT><<<ctas, kThreads, smem, s>>>(a);
-  return cudaGetLastError();
+  constexpr int fixed = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16;
+  if (const cudaError_t e = set_smem_once<tree_simt_kernel<T, D, RPT>>(fixed + tree_list_bytes(SELKV_MAX_BATCH)); e != cudaSuccess) return e;
+  return launch_chained(true, tree_simt_kernel<T, D, RPT>, dim3((unsigned)ctas), dim3(kThreads), (size_t)(fixed + tree_list_bytes(a.B)), s, a);
 }
 
 // ---- joining the pieces of a unit ----------------------------------------------------------
-// Eight rows of a unit a CTA; a thread four elements of one.  Units that one CTA finished have nothing to join.
-constexpr int kJoinRows = 8;
+// Eight rows of a unit a CTA; a thread four elements of one.  Units that one CTA finished have nothing to join.  Bound
+// by latency: the pieces' references and sums come in one round, and the first outputs with them.
+constexpr int kJoinRows = 8, kJoinAhead = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kJoinRows * D / 4) void tree_join_kernel(TreeArgs a, int unit_rows) {
-  pdl_wait();
+  constexpr int kMost = 2 * kPlanSMs;  // CTAs, and so pieces of a unit
+  __shared__ float2 ml[kMost][kJoinRows];
+  chain_begin();
   const int per = (unit_rows + kJoinRows - 1) / kJoinRows;
-  const int blk = blockIdx.x / per, r = (blockIdx.x - blk * per) * kJoinRows + threadIdx.x % kJoinRows;
+  const int blk = blockIdx.x / per, lr = threadIdx.x % kJoinRows, r = (blockIdx.x - blk * per) * kJoinRows + lr;
   const int d4 = threadIdx.x / kJoinRows, kv = blockIdx.y, b = blockIdx.z;
-  const int lo = a.before[b], tiles = (a.before[b + 1] - lo) / (a.Hkv * a.blocks), share = a.before[a.B + 1];
-  if (tiles == 0) return;
-  const int u0 = lo + (kv * a.blocks + blk) * tiles, u1 = u0 + tiles;
-  const int c0 = u0 / share, c1 = (u1 - 1) / share;
-  const int row = blk * unit_rows + r;
-  int n = a.counts != nullptr ? a.counts[b] : a.T;
-  n = min(n, a.T);
-  if (c0 == c1 || r >= unit_rows || row >= a.R || row % a.T >= n) return;
+  const int lo = a.before[b], share = a.before[a.B + 1], mine = (a.before[b + 1] - lo) / (a.Hkv * a.blocks);
+  if (mine == 0) return;
+  // the CTAs that hold the unit's pieces
+  const int u0 = lo + (kv * a.blocks + blk) * mine;
+  const bool piece = a.before[a.B + 2] != 0;
+  const int c0 = piece ? u0 : u0 / share, c1 = piece ? u0 + mine - 1 : (u0 + mine - 1) / share;
+  const int S = c1 - c0 + 1;
+  if (S == 1) return;
   const size_t rec = tree_record_floats(a.rec_rows, D);
   // the first piece lies in its CTA's second record, the others in their CTAs' first
-  auto record = [&](int c) { return a.partial + (size_t)(c * 2 + (c == c0 ? 1 : 0)) * rec; };
-  // (the unit's first tile may be its CTA's first: the record is the second all the same)
+  auto record = [&](int t) { return a.partial + (size_t)((c0 + t) * 2 + (t == 0 ? 1 : 0)) * rec; };
+  const int row = blk * unit_rows + r, n = min(a.counts != nullptr ? a.counts[b] : a.T, a.T);
+  const bool on = r < unit_rows && row < a.R && row % a.T < n;
+  auto out_of = [&](int t) {
+    return on && t < S ? __ldcg(reinterpret_cast<const float4*>(record(t)) + (size_t)d4 * a.rec_rows + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  float4 v[kJoinAhead];
+#pragma unroll
+  for (int k = 0; k < kJoinAhead; ++k) v[k] = out_of(k);
+  for (int t = d4; t < S; t += D / 4)
+    ml[t][lr] = on ? __ldcg(reinterpret_cast<const float2*>(record(t) + (size_t)a.rec_rows * D) + r) : make_float2(-INFINITY, 0.f);
+  __syncthreads();
   float M = -INFINITY;
-#pragma unroll 8
-  for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(record(c) + (size_t)a.rec_rows * D) + r).x);
+  for (int t = 0; t < S; ++t) M = fmaxf(M, ml[t][lr].x);
   const float ref = M == -INFINITY ? 0.f : M;
   float L = 0.f;
   float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int c = c0; c <= c1; ++c) {
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(record(c) + (size_t)a.rec_rows * D) + r);
-    const float4 v = __ldcg(reinterpret_cast<const float4*>(record(c)) + (size_t)d4 * a.rec_rows + r);
-    const float w = exp2f(ml.x - ref);
-    L = fmaf(ml.y, w, L);
-    // (a piece without weight has outputs 0)
-    x[0] = fmaf(v.x, w, x[0]);
-    x[1] = fmaf(v.y, w, x[1]);
-    x[2] = fmaf(v.z, w, x[2]);
-    x[3] = fmaf(v.w, w, x[3]);
+  for (int t0 = 0; t0 < S; t0 += kJoinAhead) {
+#pragma unroll
+    for (int k = 0; k < kJoinAhead; ++k) {
+      if (t0 + k < S) {
+        const float2 e = ml[t0 + k][lr];
+        const float w = exp2f(e.x - ref);  // (a piece without weight has outputs 0)
+        L = fmaf(e.y, w, L);
+        x[0] = fmaf(v[k].x, w, x[0]);
+        x[1] = fmaf(v[k].y, w, x[1]);
+        x[2] = fmaf(v[k].z, w, x[2]);
+        x[3] = fmaf(v[k].w, w, x[3]);
+      }
+      v[k] = out_of(t0 + kJoinAhead + k);
+    }
   }
+  if (!on) return;
   const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] *= inv;

@@ -1,13 +1,13 @@
 // Compensated attention of a tree of drafted tokens over a bf16 cache, on the 5th-generation tensor cores.
 //
 // The R = G T query rows of a KV head are the 128 rows of an accumulator (two accumulators above 128), so the
-// cache is read once for all of them.  Per key tile: S = Q K^T into tensor memory, the softmax warps read a row
+// cache is read once for all of them.  Per tile of 64 keys: S = Q K^T into tensor memory, the softmax warps read a row
 // each (a thread a row: no exchange for the maximum), write P = 2^(s - ref) back over S as bf16, and O += P V takes P
 // from there.  V lies in shared memory as it came, keys by d, and is the MN-major operand.
 //
-// Two such chains run side by side, each with its S, P and O, so the tensor cores work on one while the other is in its
-// softmax: with up to 128 rows they take every other key tile of a piece and are joined at its end, above it they take
-// 128 rows each of the same tiles.  The reference is a running maximum that moves only when a tile's maximum
+// Two such chains run side by side, each with its O and two places for S and P, so that a chain's next S is there when
+// its softmax ends: with up to 128 rows they take every other key tile of a piece and are joined at its end, above it
+// they take 128 rows each of the same tiles.  The reference is a running maximum that moves only when a tile's maximum
 // passes it by more than 8 (a factor of 256, far inside the range of bf16 and fp32): O is rescaled in those tiles alone.
 //
 // Arithmetic per byte is 4 R d / (4 d) = R operations: with up to 256 rows the cache's bytes bound it (281 a byte at the
@@ -18,12 +18,8 @@ namespace selkv {
 namespace {
 
 constexpr int kKeys = kTreeTcKeys;
-constexpr int kSoftWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kThreads = 384;
-constexpr int kBox = 32;       // rows of a copy
-// Registers: a softmax thread holds a row of 128 logits.  384 threads start with 168 each; the two softmax warpgroups take
-// 216 of them and the third keeps 72 (together what the launch had).
-constexpr int kSoftRegs = 216, kIssueRegs = 72;
-static_assert(2 * kSoftRegs + kIssueRegs == 3 * 168, "the launch's registers");
+constexpr int kSoftWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kTreeWarp = 11, kThreads = 384;  // (an MMA warp a chain)
+constexpr int kBox = 32;       // rows of a copy where a tile is not whole
 constexpr int kTmemCols = 512;
 constexpr float kSlack = 8.f;  // how far a maximum may pass the reference, in powers of two
 
@@ -32,35 +28,54 @@ struct Cfg {
   static constexpr int kHalves = D / 64;           // 128-byte wide halves of a row
   static constexpr int kSlot = kKeys * D * 2;      // a tile of K or V
   static constexpr int kQ = 128 * MT * D * 2;
-  static constexpr int kSlots = D == 128 ? (MT == 1 ? 5 : 4) : 8;
-  // barriers | bias of a tile, a copy a warp | (reference, sum) of the chains' rows | ancestors | parents | unfit tokens
-  static constexpr int kBars = 0, kBias = 256, kMl = kBias + kSoftWarps * kKeys * 4, kSeen = kMl + 2 * 128 * 8,
-                       kUp = kSeen + SELKV_MAX_TREE * 16, kBad = kUp + SELKV_MAX_TREE, kBefore = kBad + 16;
-  static constexpr int kFixed = 1024 + kQ + kSlots * kSlot + kBefore;
-  static_assert(kFixed + (SELKV_MAX_BATCH + 1) * 4 <= 232448, "227 KB of shared memory");
-  static_assert((2 * kSlots + 9) * 8 + 8 <= 256, "barriers and flags");
+  // Rings of K and V tiles: one for each set of tiles that is consumed in order (a chain's own, or what both take), so that
+  // every wait for a copy comes after the one for the last copy in its place: a phase later would read as done.
+  static constexpr int kRings = MT == 1 ? 2 : 1;
+  static constexpr int kRing = (D == 128 ? (MT == 1 ? 10 : 8) : 16) / kRings;  // places of a ring
+  static constexpr int kSlots = kRings * kRing;
+  // barriers | bias of a tile, a copy a warp | sums and references of the chains' rows | ancestors, parents and unfit
+  // tokens, twice | the list
+  static constexpr int kBars = 0, kBias = 512, kSum = kBias + kSoftWarps * kKeys * 4, kSeen = kSum + 2 * 128 * 8,
+                       kUp = kSeen + 2 * SELKV_MAX_TREE * 16, kBad = kUp + SELKV_MAX_TREE, kList = kBad + 2 * 16;
+  static constexpr int kFixed = 1024 + kQ + kSlots * kSlot + kList;
+  static_assert(kFixed + tree_list_bytes(SELKV_MAX_BATCH) <= 232448, "227 KB of shared memory");
+  static_assert((2 * kSlots + 20) * 8 + 8 <= 512, "barriers and flags");
 };
+// Shared-memory matrix descriptors, 128-byte swizzling, 8 rows of 128 bytes an atom: the upper word is the same for
+// all operands here; the lower one holds the address and, for the MN-major V, the distance to the next 64 elements of N.
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t next_n = 16) { return addr >> 4 | (next_n >> 4) << 16; }
+constexpr uint32_t kBMnMajor = 1u << 16;
 
-// D (fp32, tensor memory) += A (bf16 pairs, tensor memory) * B (shared memory).
-__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// The MMA warp runs as one and its elected lane issues: operands stay uniform (with the loops in one thread an
+// instruction took about 120 cycles to issue, twice what it runs).
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t l;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(l));
+  return l;
+}
+// D (fp32, tensor memory) (+)= A B with A and B in shared memory, and with A (bf16 pairs) in tensor memory.
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n .reg .pred p, l;\n .reg .b64 da, db;\n setp.ne.b32 l, %5, 0;\n setp.ne.b32 p, %4, 0;\n mov.b64 da, {%1, %6};\n"
+      " mov.b64 db, {%2, %6};\n @l tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(leader), "n"(kDescHi)
       : "memory");
 }
-// Descriptor of an MN-major operand written by TMA with 128-byte swizzling: rows of 64 elements of N, 8 rows of K an
-// atom of 1024 bytes; `next_n` bytes to the next 64 elements of N.
-__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t addr, uint32_t next_n) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(next_n >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, l;\n .reg .b64 db;\n setp.ne.b32 l, %5, 0;\n setp.ne.b32 p, %4, 0;\n mov.b64 db, {%2, %6};\n"
+      " @l tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}\n" ::"r"(d),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(leader), "n"(kDescHi)
+      : "memory");
 }
-constexpr uint32_t kBMnMajor = 1u << 16;
+__device__ __forceinline__ void commit_to(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred l;\n setp.ne.b32 l, %1, 0;\n"
+      " @l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)),
+      "r"(leader)
+      : "memory");
+}
 
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t taddr, float (&v)[32]) {
   asm volatile(
@@ -91,23 +106,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&f)[32]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t u[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(f[h * 16 + i]);
-    tmem_st16(taddr + h * 16, u);
-  }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Place in the ring (a count over the piece's copies) of K and V of tile i of n: one chain of tiles behind the other
-// has the next tile's K before this one's V.
+// Place in the ring (a count over the piece's copies) of K and V of the ring's tile i of n: the first two K, then a V and
+// the next K in turn.
+constexpr int kAhead = 2;
+__device__ __forceinline__ int k_place(int i) { return i + max(0, i - kAhead + 1); }
+__device__ __forceinline__ int v_place(int i, int n) { return i + min(i + kAhead, n); }
+// Tiles of a piece of n that chain c takes (MT 1: every other one).
 template <int MT>
-__device__ __forceinline__ int k_place(int i) { return MT == 1 ? (i == 0 ? 0 : 2 * i - 1) : 2 * i; }
-template <int MT>
-__device__ __forceinline__ int v_place(int i, int n) { return MT == 1 ? (i == n - 1 ? 2 * n - 1 : 2 * i + 2) : 2 * i + 1; }
+__device__ __forceinline__ int chain_tiles(int n, int c) { return MT == 1 ? (n + 1 - c) >> 1 : n; }
 
 __device__ __forceinline__ bool unfit16(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
 
@@ -115,48 +128,57 @@ template <int D, int MT>
 __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                                                               const __grid_constant__ CUtensorMap tmK,
                                                               const __grid_constant__ CUtensorMap tmV,
+                                                              const __grid_constant__ CUtensorMap tmK32,
+                                                              const __grid_constant__ CUtensorMap tmV32,
                                                               const __grid_constant__ CUtensorMap tmKn,
                                                               const __grid_constant__ CUtensorMap tmVn, TreeArgs a) {
   using C = Cfg<D, MT>;
-  constexpr int kSlots = C::kSlots;
+  constexpr int kRing = C::kRing;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* Qs = smem;              // [halves][128 MT rows][128 B]
-  unsigned char* ring = Qs + C::kQ;      // [slots][halves][128 keys][128 B]
-  unsigned char* misc = ring + kSlots * C::kSlot;
+  unsigned char* ring = Qs + C::kQ;      // [rings][places][halves][keys][128 B]
+  unsigned char* misc = ring + C::kSlots * C::kSlot;
   uint64_t* full = reinterpret_cast<uint64_t*>(misc + C::kBars);
-  uint64_t* empty = full + kSlots;
-  uint64_t* sfull = empty + kSlots;  // [2] S of a chain is there
-  uint64_t* pfull = sfull + 2;       // [2] its P is
-  uint64_t* ofull = pfull + 2;       // [2] its O of the piece is done
+  uint64_t* empty = full + C::kSlots;
+  uint64_t* sfull = empty + C::kSlots;  // [chain][2] S is there
+  uint64_t* pfull = sfull + 4;       // [chain][2] P is
+  uint64_t* odone = pfull + 4;       // [chain] a tile's P V is in O
+  uint64_t* ofull = odone + 2;       // [chain] its last one of a piece
   uint64_t* qfull = ofull + 2;
   uint64_t* qfree = qfull + 1;
-  uint64_t* done = qfree + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  uint64_t* done = qfree + 1;        // [chain]
+  uint64_t* tfull = done + 2;        // [2] a piece's ancestors are there
+  uint64_t* tfree = tfull + 2;       // [2] they are read
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tfree + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* bias_s = reinterpret_cast<float*>(misc + C::kBias);
-  float2* ml_s = reinterpret_cast<float2*>(misc + C::kMl);
-  uint4* seen = reinterpret_cast<uint4*>(misc + C::kSeen);
+  float2* sum_s = reinterpret_cast<float2*>(misc + C::kSum);  // [chain][128] (reference, sum)
+  uint4* seen_s = reinterpret_cast<uint4*>(misc + C::kSeen);
   int8_t* up = reinterpret_cast<int8_t*>(misc + C::kUp);
-  uint32_t* bad = reinterpret_cast<uint32_t*>(misc + C::kBad);
-  int32_t* before = reinterpret_cast<int32_t*>(misc + C::kBefore);
+  uint32_t* bad_s = reinterpret_cast<uint32_t*>(misc + C::kBad);
+  const TreeList list = tree_list_at(misc + C::kList, a.B);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_launch_dependents();
   if (threadIdx.x == kProducerWarp * 32) {
-    for (int i = 0; i < kSlots; ++i) {
+    for (int i = 0; i < C::kSlots; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&empty[i], MT);  // (the chains that take a tile)
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&sfull[i], 1);
+      mbar_init(&pfull[i], kSoftWarps / 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sfull[i], 1);
-      mbar_init(&pfull[i], 4);
+      mbar_init(&odone[i], 1);
       mbar_init(&ofull[i], 1);
+      mbar_init(&tfull[i], 1);
+      mbar_init(&done[i], 1);
+      mbar_init(&tfree[i], kSoftWarps);
     }
     mbar_init(qfull, 1);
-    mbar_init(qfree, 1);
-    mbar_init(done, 1);
+    mbar_init(qfree, 2);
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&tmQ);
@@ -167,41 +189,43 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   }
   __syncwarp();
   if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
-  tree_list<kKeys>(a, before, blockIdx.x == 0);
-  const int total = before[a.B], share = tree_share(total, gridDim.x);
-  if (blockIdx.x == 0) {
-    for (int b = threadIdx.x; b <= a.B; b += kThreads) a.before[b] = before[b];
-    if (threadIdx.x == 0) a.before[a.B + 1] = share;
-  }
+  chain_begin();
+  tree_list<kKeys>(a, list, gridDim.x, blockIdx.x == 0);
+  if (blockIdx.x == 0) tree_list_store(a, list);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int pos0 = (int)min((long long)total, (long long)blockIdx.x * share), end = min(total, pos0 + share);
+  const TreeRange range = tree_range(a, list, blockIdx.x);
 
-  if (warp >= kSoftWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
   if (warp == kProducerWarp) {
     if (lane == 0) {
-      int used = 0, pieces = 0;  // copies into the ring, pieces
+      int used[2] = {0, 0}, pieces = 0;  // copies into the rings, pieces
       bool ok = true;
-      for (int pos = pos0; ok && pos < end; ++pieces) {
-        const TreePiece p = tree_piece<kKeys>(a, before, pos, end);
-        pos += p.count;
-        const int bk = p.b * a.Hkv + p.kv, cache_tiles = (p.L + kKeys - 1) / kKeys;
+      for (TreeRange at = range; ok && at.pos < at.end; ++pieces) {
+        const TreePiece p = tree_piece<kKeys>(a, list, at);
+        at.pos += p.places;
+        const int n = p.count, bk = p.b * a.Hkv + p.kv, cache_tiles = (p.L + kKeys - 1) / kKeys;
         // K (or V) of the piece's tile i
         auto load = [&](bool v, int i) -> bool {
-          const int t = p.first + i, slot = used % kSlots;
+          const int t = p.first + i;
           const bool drafts = t >= cache_tiles;
-          const int keys = drafts ? p.n : min(kKeys, p.L - t * kKeys), boxes = (keys + kBox - 1) / kBox;
-          const int row = drafts ? bk * a.T : bk * a.m_cap + t * kKeys;
-          const CUtensorMap* map = drafts ? (v ? &tmVn : &tmKn) : (v ? &tmV : &tmK);
-          if (used >= kSlots && (!mbar_wait(&empty[slot], ((used / kSlots) & 1) ^ 1) || *abort_flag)) return false;
+          const int key0 = (drafts ? t - cache_tiles : t) * kKeys, keys = min(kKeys, (drafts ? p.n : p.L) - key0);
+          const int row = bk * (drafts ? a.T : a.m_cap) + key0, boxes = (keys + kBox - 1) / kBox;
+          const int ri = C::kRings == 2 ? i & 1 : 0, u = used[ri], slot = ri * kRing + u % kRing;
+          if (u >= kRing && (!mbar_wait(&empty[slot], ((u / kRing) & 1) ^ 1) || *abort_flag)) return false;
           mbar_arrive_expect_tx(&full[slot], (uint32_t)boxes * kBox * D * 2);
-          for (int h = 0; h < C::kHalves; ++h)
-            for (int x = 0; x < boxes; ++x)
-              tma_load_2d(ring + slot * C::kSlot + h * (kKeys * 128) + x * (kBox * 128), map, h * 64, row + x * kBox, &full[slot]);
-          ++used;
+          unsigned char* to = ring + slot * C::kSlot;
+          if (boxes == kKeys / kBox && !drafts) {
+#pragma unroll
+            for (int h = 0; h < C::kHalves; ++h) tma_load_2d(to + h * (kKeys * 128), v ? &tmV : &tmK, h * 64, row, &full[slot]);
+          } else {
+            const CUtensorMap* map = drafts ? (v ? &tmVn : &tmKn) : (v ? &tmV32 : &tmK32);
+            for (int h = 0; h < C::kHalves; ++h)
+              for (int x = 0; x < boxes; ++x)
+                tma_load_2d(to + h * (kKeys * 128) + x * (kBox * 128), map, h * 64, row + x * kBox, &full[slot]);
+          }
+          ++used[ri];
           return true;
         };
         ok = load(false, 0);
@@ -215,12 +239,11 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             for (int x = 0; x < boxes; ++x)
               tma_load_2d(Qs + h * (128 * MT * 128) + x * (kBox * 128), &tmQ, h * 64, row + x * kBox, qfull);
         }
-        if (MT == 1) {
-          for (int i = 1; ok && i < p.count; ++i) ok = load(false, i) && load(true, i - 1);
-          ok = ok && load(true, p.count - 1);
-        } else {
-          ok = load(true, 0);
-          for (int i = 1; ok && i < p.count; ++i) ok = load(false, i) && load(true, i);
+        constexpr int kFirst = kAhead * C::kRings;
+        for (int i = 1; ok && i < min(kFirst, n); ++i) ok = load(false, i);
+        for (int i = 0; ok && i < n; ++i) {
+          ok = load(true, i);
+          if (ok && i + kFirst < n) ok = load(false, i + kFirst);
         }
       }
       if (!ok) {
@@ -228,197 +251,199 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
       }
       // no copy of this CTA is in flight when it ends
-      for (int t = max(0, used - kSlots); t < used; ++t) mbar_wait(&full[t % kSlots], (t / kSlots) & 1);
+      for (int ri = 0; ri < C::kRings; ++ri)
+        for (int u = max(0, used[ri] - kRing); u < used[ri]; ++u) mbar_wait(&full[ri * kRing + u % kRing], (u / kRing) & 1);
       if (!ok && pieces > 0) mbar_wait(qfull, (pieces - 1) & 1);
     }
-  } else if (warp == kMmaWarp) {
-    if (lane == 0 && pos0 < end) {
+  } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+    // ---------------- matrix products of chain c ----------------
+    if (range.pos < range.end) {
+      const int c = warp - kMmaWarp;
       bool ok = true;
-      const uint32_t qbase = smem_u32(Qs), rbase = smem_u32(ring);
-      int base = 0, pieces = 0;  // ring places before the piece, pieces
-      int cnt[2] = {0, 0};       // tiles of each chain
-      for (int pos = pos0; ok && pos < end; ++pieces) {
-        const TreePiece p = tree_piece<kKeys>(a, before, pos, end);
-        pos += p.count;
+      const uint32_t leader = elect_one();
+      const uint32_t qbase = desc_lo(smem_u32(Qs)) + (MT == 2 ? c * (128 * 128 >> 4) : 0), rbase = smem_u32(ring);
+      const uint32_t o = tmem + 256 + c * 128;
+      int base = 0, pieces = 0, cnt = 0;  // copies into the chain's ring before the piece; pieces; tiles of the chain whose P V is issued
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        ok = __all_sync(0xffffffffu, !*abort_flag && mbar_wait(bar, parity) && !*abort_flag);
+        return ok;
+      };
+      for (TreeRange at = range; ok && at.pos < at.end; ++pieces) {
+        const TreePiece p = tree_piece<kKeys>(a, list, at);
+        at.pos += p.places;
         const int n = p.count, cache_tiles = (p.L + kKeys - 1) / kKeys;
-        const bool two = MT == 2 && a.R - p.blk * 256 > 128;  // (rows for the second accumulator)
+        const bool on = MT == 1 || c == 0 || a.R - p.blk * 256 > 128;  // (rows for the second accumulator)
         auto cols = [&](int i) {
-          const int t = p.first + i, keys = t >= cache_tiles ? p.n : min(kKeys, p.L - t * kKeys);
-          return (keys + 31) / 32 * 32;
+          const int t = p.first + i, keys = t >= cache_tiles ? p.n - (t - cache_tiles) * kKeys : p.L - t * kKeys;
+          return (min(kKeys, keys) + 31) / 32 * 32;
         };
-        auto wait_slot = [&](int place) {
-          const int u = base + place;
-          ok = ok && mbar_wait(&full[u % kSlots], (u / kSlots) & 1) && !*abort_flag;
-          return rbase + (uint32_t)(u % kSlots) * C::kSlot;
-        };
-        auto release = [&](int place) { umma_commit(&empty[(base + place) % kSlots]); };
-        auto qk = [&](int i, int c, uint32_t kaddr) {
-          const uint32_t idesc = umma_idesc_bf16(128, cols(i));
-          tc_fence_after();
+        if (!wait(qfull, pieces & 1)) break;
+        // round i: P V of the chain's tile i, whose P the softmax gives, and S of tile i + kAhead in its place; the rounds
+        // before the first tile bring the first S's
+        const int nc = chain_tiles<MT>(n, c);
+        auto tile = [&](int i) { return MT == 1 ? 2 * i + c : i; };  // of the piece
+        const int r0 = (C::kRings == 2 ? c : 0) * kRing;
+        for (int i = -kAhead; i < nc; ++i) {
+          if (i >= 0) {
+            const int u = base + v_place(i, nc), slot = r0 + u % kRing;
+            if (!wait(&full[slot], (u / kRing) & 1)) break;
+            if (on) {
+              const uint32_t s = (cnt & 1) * 64;
+              if (!wait(&pfull[c * 2 + (cnt & 1)], (cnt >> 1) & 1)) break;
+              const uint32_t idesc = umma_idesc_bf16(128, D) | kBMnMajor, v0 = desc_lo(rbase + slot * C::kSlot, kKeys * 128);
+              const uint32_t p0 = tmem + c * 128 + s;
+              const int steps = cols(tile(i)) / 16;
+              tc_fence_after();
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t qoff = (ks >> 2) * (128 * MT * 128) + (ks & 3) * 32 + (MT == 2 ? c * 128 * 128 : 0);
-            const uint32_t koff = (ks >> 2) * (kKeys * 128) + (ks & 3) * 32;
-            umma_bf16(tmem + c * 128, umma_desc_sw128(qbase + qoff), umma_desc_sw128(kaddr + koff), idesc, ks > 0);
-          }
-          umma_commit(&sfull[c]);
-        };
-        auto pv = [&](int i, int c, uint32_t vaddr, bool first, bool last) {
-          ok = ok && mbar_wait(&pfull[c], cnt[c] & 1) && !*abort_flag;
-          if (!ok) return;
-          ++cnt[c];
-          const uint32_t idesc = umma_idesc_bf16(128, D) | kBMnMajor;
-          const int steps = cols(i) / 16;
-          tc_fence_after();
-          for (int ks = 0; ks < steps; ++ks)
-            umma_bf16_ta(tmem + 256 + c * 128, tmem + c * 128 + ks * 8, umma_desc_mn_sw128(vaddr + ks * 2048, kKeys * 128), idesc,
-                         !first || ks > 0);
-          if (last) umma_commit(&ofull[c]);
-        };
-        ok = mbar_wait(qfull, pieces & 1) && !*abort_flag;
-        if (MT == 1) {
-          for (int i = 0; ok && i <= n; ++i) {
-            if (i < n) {
-              const uint32_t k = wait_slot(k_place<MT>(i));
-              if (!ok) break;
-              qk(i, i & 1, k);
-              release(k_place<MT>(i));
-              if (i == n - 1) umma_commit(qfree);
+              for (int ks = 0; ks < kKeys / 16; ++ks)
+                if (ks < steps) mma_ts(leader, o, p0 + ks * 8, v0 + ks * (2048 >> 4), idesc, ks > 0 ? 1u : (i == 0 ? 0u : 1u));
+              ++cnt;
+              commit_to(leader, &odone[c]);
+              if (i + 1 == nc) commit_to(leader, &ofull[c]);
             }
-            if (i > 0) {
-              const uint32_t v = wait_slot(v_place<MT>(i - 1, n));
-              if (!ok) break;
-              pv(i - 1, (i - 1) & 1, v, i <= 2, i - 1 >= n - 2);
-              if (!ok) break;
-              release(v_place<MT>(i - 1, n));
+            commit_to(leader, &empty[slot]);  // (a chain that is off has nothing under way)
+          }
+          const int k = i + kAhead;
+          if (k < nc) {
+            const int u = base + k_place(k), slot = r0 + u % kRing;
+            if (!wait(&full[slot], (u / kRing) & 1)) break;
+            if (on) {
+              const int j = cnt + (i >= 0 ? 1 : k);  // the chain's tile, over all pieces
+              const uint32_t idesc = umma_idesc_bf16(128, cols(tile(k))), k0 = desc_lo(rbase + slot * C::kSlot);
+              const uint32_t d = tmem + c * 128 + (j & 1) * 64;
+              tc_fence_after();
+#pragma unroll
+              for (int ks = 0; ks < D / 16; ++ks)
+                mma_ss(leader, d, qbase + (((ks >> 2) * (128 * MT * 128) + (ks & 3) * 32) >> 4),
+                       k0 + (((ks >> 2) * (kKeys * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
+              commit_to(leader, &sfull[c * 2 + (j & 1)]);
             }
+            commit_to(leader, &empty[slot]);
           }
-        } else if (ok) {
-          uint32_t k = wait_slot(k_place<MT>(0));
-          if (ok) {
-            qk(0, 0, k);
-            if (two) qk(0, 1, k);
-            release(k_place<MT>(0));
-            if (n == 1) umma_commit(qfree);
-          }
-          for (int i = 0; ok && i < n; ++i) {
-            const uint32_t v = wait_slot(v_place<MT>(i, n));
-            if (!ok) break;
-            for (int c = 0; ok && c < (two ? 2 : 1); ++c) {
-              pv(i, c, v, i == 0, i == n - 1);
-              if (!ok) break;
-              const bool last = c == (two ? 1 : 0);
-              if (last) release(v_place<MT>(i, n));
-              if (i + 1 < n) {
-                if (c == 0) k = wait_slot(k_place<MT>(i + 1));
-                if (!ok) break;
-                qk(i + 1, c, k);
-                if (last) {
-                  release(k_place<MT>(i + 1));
-                  if (i + 1 == n - 1) umma_commit(qfree);
-                }
-              }
-            }
-          }
+          if (i == nc - 1 - kAhead || (nc == 0 && i == -1)) commit_to(leader, qfree);  // the last S that there is
         }
-        base += 2 * n;
+        base += 2 * nc;
       }
-      if (!ok) {
+      if (!ok && leader) {
         *abort_flag = 1;
         raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
       }
-      umma_commit(done);  // every MMA issued above has completed once this arrives
-      mbar_wait(done, 0);
+      commit_to(leader, &done[c]);  // every MMA issued above has completed once this arrives
+      mbar_wait(&done[c], 0);
+      __syncwarp();
     }
-  }
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    // ---------------- softmax: chain c, lane quarter w4 of tensor memory ----------------
-    const int c = warp >> 2, w4 = warp & 3;
-    const uint32_t tl = tmem + ((uint32_t)(w4 * 32) << 16);
-    const uint32_t ts = tl + c * 128;
-    float* bw = bias_s + warp * kKeys;
-    const float sc = a.scale_log2;
-    const uint64_t sc2 = pack_f2(sc, sc);
-    auto warp_wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-      int ok = 0;
-      if (lane == 0) {
-        ok = !*abort_flag && mbar_wait(bar, parity);
-        if (!ok && !*abort_flag) {
+  } else if (warp == kTreeWarp) {
+    // ---------------- the ancestors, a piece ahead of the softmax ----------------
+    int trees = 0;
+    for (TreeRange at = range; at.pos < at.end;) {
+      const TreePiece p = tree_piece<kKeys>(a, list, at);
+      at.pos += p.places;
+      if (p.first + p.count <= (p.L + kKeys - 1) / kKeys) continue;
+      const int k = trees & 1;
+      if (trees >= 2 && (!__all_sync(0xffffffffu, mbar_wait(&tfree[k], ((trees >> 1) & 1) ^ 1) && !*abort_flag))) {
+        if (lane == 0) {
           *abort_flag = 1;
           raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
         }
+        break;
       }
-      return __shfl_sync(0xffffffffu, ok, 0) != 0;
+      if (lane < 4) bad_s[k * 4 + lane] = 0u;
+      tree_ancestors(a, p.b, p.n, seen_s + k * SELKV_MAX_TREE, up);
+      if (lane == 0) mbar_arrive(&tfull[k]);
+      ++trees;
+    }
+  } else if (warp < kSoftWarps) {
+    // ---------------- softmax: chain c, lane quarter w4 of tensor memory ----------------
+    const int c = warp >> 2, w4 = warp & 3;
+    const uint32_t tl = tmem + ((uint32_t)(w4 * 32) << 16);
+    float* bw = bias_s + warp * kKeys;
+    const float sc = a.scale_log2;
+    const bool added = a.bias != nullptr;  // the logits need the bias in (else scale and reference do at once)
+    const int rl = w4 * 32 + lane;         // this thread's row of the chain
+    const int pair_bar = 1 + w4;           // of the two chains' warps for the same lanes
+    // (the whole warp looks; one that has to give up takes the others along)
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+      const bool ok = __all_sync(0xffffffffu, !*abort_flag && mbar_wait(bar, parity));
+      if (!ok && lane == 0 && !*abort_flag) {
+        *abort_flag = 1;
+        raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
+      }
+      return ok;
     };
-    int base = 0;
-    int cnt = 0;              // tiles of this chain
-    int oc[2] = {0, 0};       // pieces that each chain had tiles of
-    for (int pos = pos0; pos < end;) {
-      const TreePiece p = tree_piece<kKeys>(a, before, pos, end);
-      pos += p.count;
+    int base = 0;        // copies into the chain's ring before the piece
+    int cnt = 0;         // tiles of the chain
+    int oc[2] = {0, 0};  // pieces that each chain had tiles of
+    int trees = 0;       // pieces with tokens' rows
+    float bnext[2];      // bias of the chain's next tile, in base 2; -inf: the key is out
+    auto fetch_bias = [&](const TreePiece& p, int i) {
+      if (!added) return;
+      const int key0 = (p.first + i) * kKeys + lane;
+      const float* bias = a.bias + ((size_t)p.b * a.Hkv + p.kv) * a.m_cap;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) bnext[k] = i < p.count && key0 + k * 32 < p.L ? bias[key0 + k * 32] * kLog2e : -INFINITY;
+    };
+    const int i0 = MT == 1 ? c : 0, step = MT == 1 ? 2 : 1;
+    TreeRange at = range;
+    if (at.pos < at.end) fetch_bias(tree_piece<kKeys>(a, list, at), i0);
+    while (at.pos < at.end) {
+      const TreePiece p = tree_piece<kKeys>(a, list, at);
+      at.pos += p.places;
+      // bias of the chain's tile behind tile i, be it the next piece's
+      auto fetch_behind = [&](int i) {
+        if (i + step < p.count || at.pos >= at.end) fetch_bias(p, i + step);
+        else fetch_bias(tree_piece<kKeys>(a, list, at), i0);
+      };
       const int n = p.count, cache_tiles = (p.L + kKeys - 1) / kKeys;
       const int row0 = p.blk * 128 * MT, rows = min(128 * MT, a.R - row0);
-      const int r = (MT == 2 ? c * 128 : 0) + w4 * 32 + lane;  // this thread's row of the block
+      const int r = (MT == 2 ? c * 128 : 0) + rl;  // this thread's row of the block
       const bool chain_on = MT == 1 || c * 128 < rows;
       const bool warp_on = (MT == 2 ? c * 128 : 0) + w4 * 32 < rows;
       const int tok = (row0 + r) % a.T;
-      const size_t bk = (size_t)p.b * a.Hkv + p.kv;
       const bool has_drafts = p.first + n > cache_tiles;
-      if (has_drafts) {
-        named_bar_sync(1, 256);  // the last piece's sets are read
-        if (threadIdx.x < 4) bad[threadIdx.x] = 0u;
-        tree_ancestors<256>(a, p.b, p.n, seen, up, threadIdx.x, 1);
-      }
-      const float* bias = a.bias != nullptr ? a.bias + bk * a.m_cap : nullptr;
+      const uint4* seen = seen_s + (trees & 1) * SELKV_MAX_TREE;
+      uint32_t* bad = bad_s + (trees & 1) * 4;
       float ref = -INFINITY, sum = 0.f;
       bool fresh = true;  // no tile of the chain yet
-      const int i0 = MT == 1 ? c : 0, step = MT == 1 ? 2 : 1;
-      float bnext[4];
-      auto fetch_bias = [&](int i) {
-        const int t = p.first + i;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int key = t * kKeys + k * 32 + lane;
-          bnext[k] = i < n && t < cache_tiles && key < p.L ? (bias != nullptr ? bias[key] * kLog2e : 0.f) : -INFINITY;
-        }
-      };
-      if (chain_on) fetch_bias(i0);
       for (int i = i0; chain_on && i < n; i += step) {
-        const int t = p.first + i;
+        const int t = p.first + i, j = cnt++;
         const bool drafts = t >= cache_tiles;
-        const int keys = drafts ? p.n : min(kKeys, p.L - t * kKeys), cols = (keys + 31) / 32 * 32;
-        // the tile's bias, and keys that are out (behind the last one, or with a bias of -inf)
-        bool out = false;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) out = out || bnext[k] == -INFINITY;
-        const bool plain = !drafts && !__any_sync(0xffffffffu, out);
-        const int key_here = w4 * 32 + lane;
-        bool gone = drafts ? key_here >= keys : false;
-        if (!drafts) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            bw[k * 32 + lane] = bnext[k];
-            if (k == w4) gone = bnext[k] == -INFINITY;
+        const int key0 = (drafts ? t - cache_tiles : t) * kKeys, keys = min(kKeys, (drafts ? p.n : p.L) - key0);
+        const int chunks = (keys + 31) >> 5;  // of 32 columns
+        const uint32_t ts = tl + c * 128 + (j & 1) * 64;
+        // no key is out (behind the last one, or with a bias of -inf), and the bias is in place
+        bool plain = !drafts && keys == kKeys;
+        if (added) {
+          plain = plain && !__any_sync(0xffffffffu, bnext[0] == -INFINITY || bnext[1] == -INFINITY);
+          if (!drafts) {
+            bw[lane] = bnext[0];
+            bw[32 + lane] = bnext[1];
           }
+          fetch_behind(i);
+        } else if (!plain && !drafts) {
+          bw[lane] = lane < keys ? 0.f : -INFINITY;
+          bw[32 + lane] = 32 + lane < keys ? 0.f : -INFINITY;
         }
         __syncwarp();
-        fetch_bias(i + step);
-        if (!plain && (MT == 1 || c == 0) && w4 * 32 < cols) {
+        if (drafts) warp_wait(&tfull[trees & 1], (trees >> 1) & 1);
+        const bool ok = warp_wait(&sfull[c * 2 + (j & 1)], (j >> 1) & 1);
+        tc_fence_after();
+        if (!plain) {
           // rows of V that have no weight become zeros, and so do elements of drafted tokens' rows that are no
-          // numbers (0 times an infinity is none): the epilogue gives those to the tokens that see them
-          const int u = base + v_place<MT>(i, n), slot = u % kSlots;
-          if (warp_wait(&full[slot], (u / kSlots) & 1)) {
-            uint4* v = reinterpret_cast<uint4*>(ring + slot * C::kSlot + key_here * 128);
-            if (gone) {
+          // numbers (0 times an infinity is none): the epilogue gives those to the tokens that see them.  (Where both
+          // chains take the tile, both do so, with the same values.)  Behind the wait for S: the copy that had V's place before is done.
+          const int u = base + v_place(MT == 1 ? i >> 1 : i, chain_tiles<MT>(n, c)), slot = (C::kRings == 2 ? c : 0) * kRing + u % kRing;
+          const int key = w4 * 16 + (lane & 15);  // a row and, with two halves of d, one of them
+          if (warp_wait(&full[slot], (u / kRing) & 1) && key < chunks * 32 && (lane >> 4) < C::kHalves) {
+            uint4* v = reinterpret_cast<uint4*>(ring + slot * C::kSlot + (lane >> 4) * (kKeys * 128) + key * 128);
+            if (drafts ? key >= keys : bw[key] == -INFINITY) {
 #pragma unroll
-              for (int h = 0; h < C::kHalves; ++h)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[h * (kKeys * 8) + e] = make_uint4(0u, 0u, 0u, 0u);
+              for (int e = 0; e < 8; ++e) v[e] = make_uint4(0u, 0u, 0u, 0u);
             } else if (drafts) {
-              bool any = false;
-              for (int e = 0; e < C::kHalves * 8; ++e) {
-                uint4 x = v[(e >> 3) * (kKeys * 8) + (e & 7)];
+#pragma unroll 1
+              for (int e = 0; e < 8; ++e) {
+                const uint4 x = v[e];
                 uint32_t w[4] = {x.x, x.y, x.z, x.w};
                 bool hit = false;
 #pragma unroll
@@ -432,82 +457,73 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
                     hit = true;
                   }
                 }
-                if (hit) v[(e >> 3) * (kKeys * 8) + (e & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
-                any = any || hit;
+                if (hit) {
+                  atomicOr(&bad[(key0 + key) >> 5], 1u << (key & 31));
+                  __threadfence_block();  // (the other chain may find the element gone)
+                }
+                v[e] = make_uint4(w[0], w[1], w[2], w[3]);
               }
-              if (any) atomicOr(&bad[key_here >> 5], 1u << (key_here & 31));
             }
           }
           fence_proxy_async_smem();
           __syncwarp();
         }
-        const bool ok = warp_wait(&sfull[c], cnt & 1);
-        ++cnt;
-        tc_fence_after();
         if (ok && warp_on) {
-          float x[4][32];
+          // the reference moves to `mx` where that passes it by more than the slack; returns what is added to the logits
+          auto settle = [&](float mx) {
+            const bool move = fresh || mx > ref + kSlack;
+            if (!fresh && __any_sync(0xffffffffu, move)) {
+              warp_wait(&odone[c], (j - 1) & 1);  // the tile before is in O (this tile's S came behind the one before that)
+              tc_fence_after();
+              const float f = move ? ex2_approx(ref - mx) : 1.f;
+              sum *= f;
+#pragma unroll 1
+              for (int d = 0; d < D; d += 16) {
+                float o[16];
+                tmem_ld16_issue(tl + 256 + c * 128 + d, o);
+                tmem_wait_ld16(o);
+                uint32_t w[16];
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (q * 32 < cols) tmem_ld32_issue(ts + q * 32, x[q]);
-          float mx = -INFINITY;
+                for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(o[e] * f);
+                tmem_st16(tl + 256 + c * 128 + d, w);
+              }
+            }
+            if (move) ref = mx;
+            fresh = false;
+            return ref == -INFINITY ? 0.f : -ref;
+          };
           if (plain) {
+            float x[2][32];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 2; ++q) tmem_ld32_issue(ts + q * 32, x[q]);
+            float mx = -INFINITY;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
               tmem_wait_ld32(x[q]);
-              const uint32_t ba = smem_u32(bw + q * 32);
+              if (added) {
+                const uint32_t ba = smem_u32(bw + q * 32);
+                const uint64_t sc2 = pack_f2(sc, sc);
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 b4 = lds_f4(ba + e * 4);
-                unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), sc2, pack_f2(b4.x, b4.y)), x[q][e], x[q][e + 1]);
-                unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), sc2, pack_f2(b4.z, b4.w)), x[q][e + 2], x[q][e + 3]);
+                for (int e = 0; e < 32; e += 4) {
+                  const float4 b4 = lds_f4(ba + e * 4);
+                  unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), sc2, pack_f2(b4.x, b4.y)), x[q][e], x[q][e + 1]);
+                  unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), sc2, pack_f2(b4.z, b4.w)), x[q][e + 2], x[q][e + 3]);
+                }
               }
               mx = fmaxf(mx, max32(x[q]));
             }
-          } else {
-            const uint4 sees = drafts ? seen[tok] : make_uint4(0u, 0u, 0u, 0u);
+            // (without a bias the scale, which is positive, goes in with the reference)
+            const float neg = settle(added ? mx : mx * sc), by = added ? 1.f : sc;
+            const uint64_t neg2 = pack_f2(neg, neg), by2 = pack_f2(by, by);
+            uint64_t s01 = pack_f2(0.f, 0.f), s23 = s01;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (q * 32 < cols) {
-                tmem_wait_ld32(x[q]);
-                const uint32_t w = q == 0 ? sees.x : q == 1 ? sees.y : q == 2 ? sees.z : sees.w;
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  const float b = drafts ? ((w >> e) & 1u ? 0.f : -INFINITY) : bw[q * 32 + e];
-                  x[q][e] = b == -INFINITY ? -INFINITY : fmaf(x[q][e], sc, b);
-                }
-                mx = fmaxf(mx, max32(x[q]));
-              }
-            }
-          }
-          const bool move = fresh ? true : mx > ref + kSlack;
-          if (!fresh && __any_sync(0xffffffffu, move)) {
-            // (the chain's O is done: this tile's S came behind it)
-            const float f = move ? ex2_approx(ref - mx) : 1.f;
-            sum *= f;
-#pragma unroll 1
-            for (int d = 0; d < D; d += 32) {
-              float o[32];
-              tmem_ld32_issue(tl + 256 + c * 128 + d, o);
-              tmem_wait_ld32(o);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] *= f;
-              tmem_st32(tl + 256 + c * 128 + d, o);
-            }
-          }
-          if (move) ref = mx;
-          fresh = false;
-          const float neg = ref == -INFINITY ? 0.f : -ref;
-          const uint64_t neg2 = pack_f2(neg, neg);
-          uint64_t s01 = pack_f2(0.f, 0.f), s23 = s01;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (q * 32 < cols) {
+            for (int q = 0; q < 2; ++q) {
               uint32_t w[16];
 #pragma unroll
               for (int e = 0; e < 32; e += 4) {
                 float y0, y1, y2, y3;
-                unpack_f2(fadd2(pack_f2(x[q][e], x[q][e + 1]), neg2), y0, y1);
-                unpack_f2(fadd2(pack_f2(x[q][e + 2], x[q][e + 3]), neg2), y2, y3);
+                unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), by2, neg2), y0, y1);
+                unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), by2, neg2), y2, y3);
                 y0 = ex2_approx(y0);
                 y1 = ex2_approx(y1);
                 y2 = ex2_approx(y2);
@@ -519,87 +535,131 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
               }
               tmem_st16(ts + q * 16, w);
             }
+            float a0, a1, a2, a3;
+            unpack_f2(s01, a0, a1);
+            unpack_f2(s23, a2, a3);
+            sum += (a0 + a1) + (a2 + a3);
+          } else {
+            // A tile with keys that are out, or of tokens: S is read twice, 16 columns at a time, in a loop that stays
+            // one (little code: it runs once or twice a unit).  P's columns lie before the ones read after it.
+            const uint32_t* sees = reinterpret_cast<const uint32_t*>(seen + tok) + (key0 >> 5);
+            float mx = -INFINITY, neg = 0.f;
+#pragma unroll 1
+            for (int k = 0; k < 4 * chunks; ++k) {
+              const int q = k < 2 * chunks ? k : k - 2 * chunks;
+              float x[16];
+              tmem_ld16_issue(ts + q * 16, x);
+              tmem_wait_ld16(x);
+              if (drafts) {
+                const uint32_t m = sees[q >> 1] >> ((q & 1) * 16);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = (m & (1u << e)) != 0u ? x[e] * sc : -INFINITY;
+              } else {
+                const uint32_t ba = smem_u32(bw + q * 16);
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                  const float4 b4 = lds_f4(ba + e * 4);
+                  const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                  for (int h = 0; h < 4; ++h) {
+                    const float y = fmaf(x[e + h], sc, b[h]);
+                    x[e + h] = b[h] == -INFINITY ? -INFINITY : y;  // (whatever the row holds)
+                  }
+                }
+              }
+              if (k < 2 * chunks) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[e]);
+                if (k == 2 * chunks - 1) neg = settle(mx);
+              } else {
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                  const float y0 = ex2_approx(x[e] + neg), y1 = ex2_approx(x[e + 1] + neg);
+                  sum += y0 + y1;
+                  w[e / 2] = pack_bf16(y0, y1);
+                }
+                tmem_st8(ts + q * 8, w);
+              }
+            }
           }
-          float a0, a1, a2, a3;
-          unpack_f2(s01, a0, a1);
-          unpack_f2(s23, a2, a3);
-          sum += (a0 + a1) + (a2 + a3);
           tmem_wait_st();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&pfull[c]);
+        if (lane == 0) mbar_arrive(&pfull[c * 2 + (j & 1)]);
       }
-      base += 2 * n;
+      if (!chain_on || i0 >= n) fetch_behind(n);
+      base += 2 * chain_tiles<MT>(n, c);
 
       // ---------------- the piece's rows ----------------
       bool ok = true;
-      float f[2] = {c == 0 ? 1.f : 0.f, c == 0 ? 0.f : 1.f};
-      bool use[2] = {MT == 1 || c == 0, MT == 1 ? n > 1 : c == 1};
+      const bool use[2] = {MT == 1 || c == 0, MT == 1 ? n > 1 : c == 1};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         if (!use[k] || !chain_on) continue;
-        ok = warp_wait(&ofull[k], oc[k] & 1) && ok;
+        if (warp_on) ok = warp_wait(&ofull[k], oc[k] & 1) && ok;  // (others might come too late for the phase)
         ++oc[k];
       }
+      if (has_drafts) ok = warp_wait(&tfull[trees & 1], (trees >> 1) & 1) && ok;
       tc_fence_after();
       if (warp_on) {
-        if (MT == 1) {
-          ml_s[c * 128 + r] = make_float2(ref, sum);
-          named_bar_sync(2 + w4, 64);
-          const float2 other = ml_s[(c ^ 1) * 128 + r];
-          const float top = fmaxf(ref, other.x), base2 = top == -INFINITY ? 0.f : top;
-          const float mine = ex2_approx(ref - base2), its = ex2_approx(other.x - base2);
-          f[c] = mine;
-          f[c ^ 1] = its;
-          sum = sum * mine + other.y * its;
+        float f[2] = {1.f, 1.f};
+        if (MT == 1) {  // the row's sum in both chains
+          sum_s[c * 128 + rl] = make_float2(ref, sum);
+          named_bar_sync(pair_bar, 64);
+          const float2 s0 = sum_s[rl], s1 = sum_s[128 + rl];
+          const float top = fmaxf(s0.x, s1.x), zero = top == -INFINITY ? 0.f : top;
+          f[0] = ex2_approx(s0.x - zero);
+          f[1] = ex2_approx(s1.x - zero);
+          sum = s0.y * f[0] + s1.y * f[1];
           ref = top;
         }
-        const int d0 = MT == 1 ? c * (D / 2) : 0, d1 = MT == 1 ? d0 + D / 2 : D;
+        constexpr int kCols = MT == 1 ? D / 2 : D;  // columns of O a warp takes
+        const int d0 = MT == 1 ? c * kCols : 0;
         const bool whole = p.whole();
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint32_t unfit[4] = {0u, 0u, 0u, 0u};
-        bool any_unfit = false;
-        if (has_drafts && (bad[0] | bad[1] | bad[2] | bad[3]) != 0u) {
+        bool any_unfit = false;  // the row sees a token whose values are not all numbers
+        if (has_drafts && tok < p.n) {
           const uint4 sees = seen[tok];
-          unfit[0] = sees.x & bad[0];
-          unfit[1] = sees.y & bad[1];
-          unfit[2] = sees.z & bad[2];
-          unfit[3] = sees.w & bad[3];
-          any_unfit = (unfit[0] | unfit[1] | unfit[2] | unfit[3]) != 0u && tok < p.n;
+          any_unfit = ((sees.x & bad[0]) | (sees.y & bad[1]) | (sees.z & bad[2]) | (sees.w & bad[3])) != 0u;
         }
         float* rec = whole ? nullptr : tree_record(a, blockIdx.x, p);
         __nv_bfloat16* orow = static_cast<__nv_bfloat16*>(a.out) + (((size_t)p.b * a.Hq + p.kv * a.G) * a.T + row0 + r) * D;
         const bool write = ok && r < rows && tok < p.n;
+        const size_t new_row = ((size_t)p.b * a.Hkv + p.kv) * a.T;
 #pragma unroll 1
-        for (int d = d0; d < d1; d += 32) {
-          float o[32];
+        for (int d = d0; d < d0 + kCols; d += 16) {
+          float o[16];
+          tmem_ld16_issue(tl + 256 + (MT == 2 ? c * 128 : 0) + d, o);
+          tmem_wait_ld16(o);
+          if (MT == 1) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+            for (int e = 0; e < 16; ++e) o[e] *= f[0];
+            if (n > 1) {
+              float y[16];
+              tmem_ld16_issue(tl + 384 + d, y);
+              tmem_wait_ld16(y);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (!use[k]) continue;
-            float y[32];
-            tmem_ld32_issue(tl + 256 + k * 128 + d, y);
-            tmem_wait_ld32(y);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = fmaf(y[e], f[k], o[e]);
+              for (int e = 0; e < 16; ++e) o[e] = fmaf(y[e], f[1], o[e]);
+            }
           }
           if (any_unfit) {
+#pragma unroll 1
             for (int u = 0; u < p.n; ++u)
-              if ((unfit[u >> 5] >> (u & 31)) & 1u) {
-                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v_new) + (bk * a.T + u) * D + d;
+              if ((reinterpret_cast<const uint32_t*>(seen + tok)[u >> 5] & bad[u >> 5]) >> (u & 31) & 1u) {
+                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.v_new) + (new_row + u) * D + d;
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  const float y = __bfloat162float(v[e]);
-                  if (!(fabsf(y) < INFINITY)) o[e] += y;
+                for (int e = 0; e < 16; ++e) {
+                  const float g = __bfloat162float(v[e]);
+                  if (!(fabsf(g) < INFINITY)) o[e] += g;
                 }
               }
           }
           if (!write) continue;
           if (whole) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
+            for (int e = 0; e < 16; e += 8) {
               uint4 w;
               w.x = pack_bf16(o[e] * inv, o[e + 1] * inv);
               w.y = pack_bf16(o[e + 2] * inv, o[e + 3] * inv);
@@ -609,13 +669,18 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
+            for (int e = 0; e < 16; e += 4)
               reinterpret_cast<float4*>(rec)[(size_t)((d + e) / 4) * a.rec_rows + r] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
         }
-        if (write && !whole && (MT == 2 || c == 0)) reinterpret_cast<float2*>(rec + (size_t)a.rec_rows * D)[r] = make_float2(ref, sum);
+        if (write && !whole && d0 == 0) reinterpret_cast<float2*>(rec + (size_t)a.rec_rows * D)[r] = make_float2(ref, sum);
         tc_fence_before();
-        if (MT == 1) named_bar_sync(2 + w4, 64);  // both chains' O and sums are read
+        if (MT == 1) named_bar_sync(pair_bar, 64);  // both chains' O, and the rows' sums, are read
+      }
+      if (has_drafts) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tfree[trees & 1]);
+        ++trees;
       }
     }
   }
@@ -628,16 +693,16 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
 template <int D, int MT>
 cudaError_t launch(const TreeArgs& a, int ctas, cudaStream_t s) {
   using C = Cfg<D, MT>;
-  CUtensorMap q, k, v, kn, vn;
+  CUtensorMap q, k, v, k32, v32, kn, vn;
   const uint64_t bk = (uint64_t)a.B * a.Hkv;
-  if (!encode_rows_bf16(&q, a.q, (uint64_t)a.B * a.Hq * a.T, D, kBox) || !encode_rows_bf16(&k, a.Kc, bk * a.m_cap, D, kBox) ||
-      !encode_rows_bf16(&v, a.Vc, bk * a.m_cap, D, kBox) || !encode_rows_bf16(&kn, a.k_new, bk * a.T, D, kBox) ||
+  if (!encode_rows_bf16(&q, a.q, (uint64_t)a.B * a.Hq * a.T, D, kBox) || !encode_rows_bf16(&k, a.Kc, bk * a.m_cap, D, kKeys) ||
+      !encode_rows_bf16(&v, a.Vc, bk * a.m_cap, D, kKeys) || !encode_rows_bf16(&k32, a.Kc, bk * a.m_cap, D, kBox) ||
+      !encode_rows_bf16(&v32, a.Vc, bk * a.m_cap, D, kBox) || !encode_rows_bf16(&kn, a.k_new, bk * a.T, D, kBox) ||
       !encode_rows_bf16(&vn, a.v_new, bk * a.T, D, kBox))
     return cudaErrorInvalidValue;
-  constexpr int most = C::kFixed + (SELKV_MAX_BATCH + 1) * 4;
-  if (const cudaError_t e = set_smem_once<tree_tc_kernel<D, MT>>(most); e != cudaSuccess) return e;
-  tree_tc_kernel<D, MT><<<ctas, kThreads, C::kFixed + (a.B + 1) * 4, s>>>(q, k, v, kn, vn, a);
-  return cudaGetLastError();
+  if (const cudaError_t e = set_smem_once<tree_tc_kernel<D, MT>>(C::kFixed + tree_list_bytes(SELKV_MAX_BATCH)); e != cudaSuccess) return e;
+  return launch_chained(true, tree_tc_kernel<D, MT>, dim3((unsigned)ctas), dim3(kThreads), C::kFixed + tree_list_bytes(a.B), s, q, k, v, k32, v32,
+                        kn, vn, a);
 }
 
 }  // namespace
