@@ -19,6 +19,7 @@ struct WsHeader {
 static_assert(sizeof(WsHeader) == 256, "header is 256 bytes");
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ void raise_flag(uint32_t* flags, uint32_t bit) { atomicOr(flags, bit); }
 

@@ -21,25 +21,32 @@ constexpr int kKeys = kTreeTcKeys;
 constexpr int kSoftWarps = 8, kProducerWarp = 8, kMmaWarp = 9, kTreeWarp = 11, kThreads = 384;  // (an MMA warp a chain)
 constexpr int kBox = 32;       // rows of a copy where a tile is not whole
 constexpr int kTmemCols = 512;
-constexpr float kSlack = 8.f;  // how far a maximum may pass the reference, in powers of two
+// A reference is at least this: rows with the lowest number for a bias, or none at all, have weight 0 beside a token's own
+// logit, and the reference's product with log2 e stays a number.
+constexpr float kLowest = -1e37f;
+constexpr float kSlack = 8.f;  // how far a maximum may pass the reference (powers of two, or of e)
 
 template <int D, int MT>
 struct Cfg {
   static constexpr int kHalves = D / 64;           // 128-byte wide halves of a row
   static constexpr int kSlot = kKeys * D * 2;      // a tile of K or V
   static constexpr int kQ = 128 * MT * D * 2;
+  // Q of the next piece is fetched behind this one's rows where there is room for it (a copy waits for some us behind those
+  // under way)
+  static constexpr int kQs = MT == 1 ? 2 : 1;
   // Rings of K and V tiles: one for each set of tiles that is consumed in order (a chain's own, or what both take), so that
   // every wait for a copy comes after the one for the last copy in its place: a phase later would read as done.
   static constexpr int kRings = MT == 1 ? 2 : 1;
-  static constexpr int kRing = (D == 128 ? (MT == 1 ? 10 : 8) : 16) / kRings;  // places of a ring
+  static constexpr int kRing = (D == 128 ? 8 : 16) / kRings;  // places of a ring
+  static_assert(kRing >= 4, "V of a tile comes at most 3 places behind its K");
   static constexpr int kSlots = kRings * kRing;
   // barriers | bias of a tile, a copy a warp | sums and references of the chains' rows | ancestors, parents and unfit
   // tokens, twice | the list
   static constexpr int kBars = 0, kBias = 512, kSum = kBias + kSoftWarps * kKeys * 4, kSeen = kSum + 2 * 128 * 8,
                        kUp = kSeen + 2 * SELKV_MAX_TREE * 16, kBad = kUp + SELKV_MAX_TREE, kList = kBad + 2 * 16;
-  static constexpr int kFixed = 1024 + kQ + kSlots * kSlot + kList;
+  static constexpr int kFixed = 1024 + kQs * kQ + kSlots * kSlot + kList;
   static_assert(kFixed + tree_list_bytes(SELKV_MAX_BATCH) <= 232448, "227 KB of shared memory");
-  static_assert((2 * kSlots + 20) * 8 + 8 <= 512, "barriers and flags");
+  static_assert((2 * kSlots + 22) * 8 + 8 <= 512, "barriers and flags");
 };
 // Shared-memory matrix descriptors, 128-byte swizzling, 8 rows of 128 bytes an atom: the upper word is the same for
 // all operands here; the lower one holds the address and, for the MN-major V, the distance to the next 64 elements of N.
@@ -137,8 +144,8 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  unsigned char* Qs = smem;              // [halves][128 MT rows][128 B]
-  unsigned char* ring = Qs + C::kQ;      // [rings][places][halves][keys][128 B]
+  unsigned char* Qs = smem;              // [kQs][halves][128 MT rows][128 B]
+  unsigned char* ring = Qs + C::kQs * C::kQ;      // [rings][places][halves][keys][128 B]
   unsigned char* misc = ring + C::kSlots * C::kSlot;
   uint64_t* full = reinterpret_cast<uint64_t*>(misc + C::kBars);
   uint64_t* empty = full + C::kSlots;
@@ -146,9 +153,9 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   uint64_t* pfull = sfull + 4;       // [chain][2] P is
   uint64_t* odone = pfull + 4;       // [chain] a tile's P V is in O
   uint64_t* ofull = odone + 2;       // [chain] its last one of a piece
-  uint64_t* qfull = ofull + 2;
-  uint64_t* qfree = qfull + 1;
-  uint64_t* done = qfree + 1;        // [chain]
+  uint64_t* qfull = ofull + 2;       // [kQs]
+  uint64_t* qfree = qfull + 2;
+  uint64_t* done = qfree + 2;        // [chain]
   uint64_t* tfull = done + 2;        // [2] a piece's ancestors are there
   uint64_t* tfree = tfull + 2;       // [2] they are read
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tfree + 2);
@@ -175,10 +182,10 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
       mbar_init(&ofull[i], 1);
       mbar_init(&tfull[i], 1);
       mbar_init(&done[i], 1);
+      mbar_init(&qfull[i], 1);
+      mbar_init(&qfree[i], 2);
       mbar_init(&tfree[i], kSoftWarps);
     }
-    mbar_init(qfull, 1);
-    mbar_init(qfree, 2);
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&tmQ);
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   }
   __syncwarp();
   if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
-  chain_begin();
+  pdl_wait();  // (no early start for what follows: its CTAs, waiting, cost this kernel 4 us of 34)
   tree_list<kKeys>(a, list, gridDim.x, blockIdx.x == 0);
   if (blockIdx.x == 0) tree_list_store(a, list);
   tc_fence_before();
@@ -202,6 +209,19 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
     if (lane == 0) {
       int used[2] = {0, 0}, pieces = 0;  // copies into the rings, pieces
       bool ok = true;
+      int asked = 0;  // pieces whose Q is
+      auto load_q = [&](const TreePiece& p) -> bool {
+        const int k = asked % C::kQs;
+        if (asked >= C::kQs && (!mbar_wait(&qfree[k], ((asked / C::kQs) & 1) ^ 1) || *abort_flag)) return false;
+        const int row0 = p.blk * 128 * MT, boxes = (min(128 * MT, a.R - row0) + kBox - 1) / kBox;
+        const int row = (p.b * a.Hq + p.kv * a.G) * a.T + row0;
+        mbar_arrive_expect_tx(&qfull[k], (uint32_t)boxes * kBox * D * 2);
+        for (int h = 0; h < C::kHalves; ++h)
+          for (int x = 0; x < boxes; ++x)
+            tma_load_2d(Qs + k * C::kQ + h * (128 * MT * 128) + x * (kBox * 128), &tmQ, h * 64, row + x * kBox, &qfull[k]);
+        ++asked;
+        return true;
+      };
       for (TreeRange at = range; ok && at.pos < at.end; ++pieces) {
         const TreePiece p = tree_piece<kKeys>(a, list, at);
         at.pos += p.places;
@@ -229,22 +249,14 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
           return true;
         };
         ok = load(false, 0);
-        if (ok && pieces > 0) ok = mbar_wait(qfree, (pieces - 1) & 1) && !*abort_flag;
-        if (!ok) break;
-        {
-          const int row0 = p.blk * 128 * MT, boxes = (min(128 * MT, a.R - row0) + kBox - 1) / kBox;
-          const int row = (p.b * a.Hq + p.kv * a.G) * a.T + row0;
-          mbar_arrive_expect_tx(qfull, (uint32_t)boxes * kBox * D * 2);
-          for (int h = 0; h < C::kHalves; ++h)
-            for (int x = 0; x < boxes; ++x)
-              tma_load_2d(Qs + h * (128 * MT * 128) + x * (kBox * 128), &tmQ, h * 64, row + x * kBox, qfull);
-        }
+        if (ok && asked == pieces) ok = load_q(p);
         constexpr int kFirst = kAhead * C::kRings;
         for (int i = 1; ok && i < min(kFirst, n); ++i) ok = load(false, i);
         for (int i = 0; ok && i < n; ++i) {
           ok = load(true, i);
           if (ok && i + kFirst < n) ok = load(false, i + kFirst);
         }
+        if (C::kQs == 2 && ok && at.pos < at.end) ok = load_q(tree_piece<kKeys>(a, list, at));
       }
       if (!ok) {
         *abort_flag = 1;
@@ -253,7 +265,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
       // no copy of this CTA is in flight when it ends
       for (int ri = 0; ri < C::kRings; ++ri)
         for (int u = max(0, used[ri] - kRing); u < used[ri]; ++u) mbar_wait(&full[ri * kRing + u % kRing], (u / kRing) & 1);
-      if (!ok && pieces > 0) mbar_wait(qfull, (pieces - 1) & 1);
+      for (int q = max(0, asked - C::kQs); q < asked; ++q) mbar_wait(&qfull[q % C::kQs], (q / C::kQs) & 1);
     }
   } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
     // ---------------- matrix products of chain c ----------------
@@ -261,7 +273,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
       const int c = warp - kMmaWarp;
       bool ok = true;
       const uint32_t leader = elect_one();
-      const uint32_t qbase = desc_lo(smem_u32(Qs)) + (MT == 2 ? c * (128 * 128 >> 4) : 0), rbase = smem_u32(ring);
+      const uint32_t q0 = desc_lo(smem_u32(Qs)) + (MT == 2 ? c * (128 * 128 >> 4) : 0), rbase = smem_u32(ring);
       const uint32_t o = tmem + 256 + c * 128;
       int base = 0, pieces = 0, cnt = 0;  // copies into the chain's ring before the piece; pieces; tiles of the chain whose P V is issued
       auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -278,7 +290,9 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
           const int t = p.first + i, keys = t >= cache_tiles ? p.n - (t - cache_tiles) * kKeys : p.L - t * kKeys;
           return (min(kKeys, keys) + 31) / 32 * 32;
         };
-        if (!wait(qfull, pieces & 1)) break;
+        const int qi = pieces % C::kQs;
+        const uint32_t qbase = q0 + qi * (C::kQ >> 4);
+        if (!wait(&qfull[qi], (pieces / C::kQs) & 1)) break;
         // round i: P V of the chain's tile i, whose P the softmax gives, and S of tile i + kAhead in its place; the rounds
         // before the first tile bring the first S's
         const int nc = chain_tiles<MT>(n, c);
@@ -321,7 +335,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             }
             commit_to(leader, &empty[slot]);
           }
-          if (i == nc - 1 - kAhead || (nc == 0 && i == -1)) commit_to(leader, qfree);  // the last S that there is
+          if (i == nc - 1 - kAhead || (nc == 0 && i == -1)) commit_to(leader, &qfree[qi]);  // the last S that there is
         }
         base += 2 * nc;
       }
@@ -358,8 +372,10 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
     const int c = warp >> 2, w4 = warp & 3;
     const uint32_t tl = tmem + ((uint32_t)(w4 * 32) << 16);
     float* bw = bias_s + warp * kKeys;
-    const float sc = a.scale_log2;
-    const bool added = a.bias != nullptr;  // the logits need the bias in (else scale and reference do at once)
+    // Without a bias the logits and the reference are in base 2, and the scale goes in with the reference.  With one they
+    // are in base e, as the bias is, and their factor to base 2 goes in with the reference.
+    const bool added = a.bias != nullptr;
+    const float sc = added ? a.scale_log2 * kLn2 : a.scale_log2, to2 = added ? kLog2e : 1.f;
     const int rl = w4 * 32 + lane;         // this thread's row of the chain
     const int pair_bar = 1 + w4;           // of the two chains' warps for the same lanes
     // (the whole warp looks; one that has to give up takes the others along)
@@ -376,13 +392,13 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
     int cnt = 0;         // tiles of the chain
     int oc[2] = {0, 0};  // pieces that each chain had tiles of
     int trees = 0;       // pieces with tokens' rows
-    float bnext[2];      // bias of the chain's next tile, in base 2; -inf: the key is out
+    float bnext[2];      // bias of the chain's next tile; -inf: the key is out
     auto fetch_bias = [&](const TreePiece& p, int i) {
       if (!added) return;
       const int key0 = (p.first + i) * kKeys + lane;
       const float* bias = a.bias + ((size_t)p.b * a.Hkv + p.kv) * a.m_cap;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) bnext[k] = i < p.count && key0 + k * 32 < p.L ? bias[key0 + k * 32] * kLog2e : -INFINITY;
+      for (int k = 0; k < 2; ++k) bnext[k] = i < p.count && key0 + k * 32 < p.L ? bias[key0 + k * 32] : -INFINITY;
     };
     const int i0 = MT == 1 ? c : 0, step = MT == 1 ? 2 : 1;
     TreeRange at = range;
@@ -412,32 +428,29 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         const int key0 = (drafts ? t - cache_tiles : t) * kKeys, keys = min(kKeys, (drafts ? p.n : p.L) - key0);
         const int chunks = (keys + 31) >> 5;  // of 32 columns
         const uint32_t ts = tl + c * 128 + (j & 1) * 64;
-        // no key is out (behind the last one, or with a bias of -inf), and the bias is in place
+        // no key is out (behind the last one, or with a bias of -inf)
         bool plain = !drafts && keys == kKeys;
         if (added) {
           plain = plain && !__any_sync(0xffffffffu, bnext[0] == -INFINITY || bnext[1] == -INFINITY);
-          if (!drafts) {
-            bw[lane] = bnext[0];
-            bw[32 + lane] = bnext[1];
-          }
+          bw[lane] = bnext[0];
+          bw[32 + lane] = bnext[1];
           fetch_behind(i);
-        } else if (!plain && !drafts) {
-          bw[lane] = lane < keys ? 0.f : -INFINITY;
-          bw[32 + lane] = 32 + lane < keys ? 0.f : -INFINITY;
+          __syncwarp();
         }
-        __syncwarp();
         if (drafts) warp_wait(&tfull[trees & 1], (trees >> 1) & 1);
-        const bool ok = warp_wait(&sfull[c * 2 + (j & 1)], (j >> 1) & 1);
+        bool ok = warp_wait(&sfull[c * 2 + (j & 1)], (j >> 1) & 1);
         tc_fence_after();
         if (!plain) {
           // rows of V that have no weight become zeros, and so do elements of drafted tokens' rows that are no
           // numbers (0 times an infinity is none): the epilogue gives those to the tokens that see them.  (Where both
-          // chains take the tile, both do so, with the same values.)  Behind the wait for S: the copy that had V's place before is done.
+          // chains take the tile, both do so, with the same values.)  Behind the wait for S: the copy that had V's place
+          // before is done.
           const int u = base + v_place(MT == 1 ? i >> 1 : i, chain_tiles<MT>(n, c)), slot = (C::kRings == 2 ? c : 0) * kRing + u % kRing;
+          ok = warp_wait(&full[slot], (u / kRing) & 1) && ok;
           const int key = w4 * 16 + (lane & 15);  // a row and, with two halves of d, one of them
-          if (warp_wait(&full[slot], (u / kRing) & 1) && key < chunks * 32 && (lane >> 4) < C::kHalves) {
+          if (ok && key < chunks * 32 && (lane >> 4) < C::kHalves) {
             uint4* v = reinterpret_cast<uint4*>(ring + slot * C::kSlot + (lane >> 4) * (kKeys * 128) + key * 128);
-            if (drafts ? key >= keys : bw[key] == -INFINITY) {
+            if (key >= keys || (added && !drafts && bw[key] == -INFINITY)) {
 #pragma unroll
               for (int e = 0; e < 8; ++e) v[e] = make_uint4(0u, 0u, 0u, 0u);
             } else if (drafts) {
@@ -471,11 +484,12 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         if (ok && warp_on) {
           // the reference moves to `mx` where that passes it by more than the slack; returns what is added to the logits
           auto settle = [&](float mx) {
+            mx = fmaxf(mx, kLowest);
             const bool move = fresh || mx > ref + kSlack;
             if (!fresh && __any_sync(0xffffffffu, move)) {
               warp_wait(&odone[c], (j - 1) & 1);  // the tile before is in O (this tile's S came behind the one before that)
               tc_fence_after();
-              const float f = move ? ex2_approx(ref - mx) : 1.f;
+              const float f = move ? ex2_approx((ref - mx) * to2) : 1.f;
               sum *= f;
 #pragma unroll 1
               for (int d = 0; d < D; d += 16) {
@@ -490,7 +504,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             }
             if (move) ref = mx;
             fresh = false;
-            return ref == -INFINITY ? 0.f : -ref;
+            return -ref * to2;
           };
           if (plain) {
             float x[2][32];
@@ -513,7 +527,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
               mx = fmaxf(mx, max32(x[q]));
             }
             // (without a bias the scale, which is positive, goes in with the reference)
-            const float neg = settle(added ? mx : mx * sc), by = added ? 1.f : sc;
+            const float neg = settle(added ? mx : mx * sc), by = added ? kLog2e : sc;
             const uint64_t neg2 = pack_f2(neg, neg), by2 = pack_f2(by, by);
             uint64_t s01 = pack_f2(0.f, 0.f), s23 = s01;
 #pragma unroll
@@ -555,16 +569,24 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[e] = (m & (1u << e)) != 0u ? x[e] * sc : -INFINITY;
               } else {
-                const uint32_t ba = smem_u32(bw + q * 16);
+                float b[16];
+                if (added) {
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                  const float4 b4 = lds_f4(ba + e * 4);
-                  const float b[4] = {b4.x, b4.y, b4.z, b4.w};
-#pragma unroll
-                  for (int h = 0; h < 4; ++h) {
-                    const float y = fmaf(x[e + h], sc, b[h]);
-                    x[e + h] = b[h] == -INFINITY ? -INFINITY : y;  // (whatever the row holds)
+                  for (int e = 0; e < 16; e += 4) {
+                    const float4 b4 = lds_f4(smem_u32(bw + q * 16 + e));
+                    b[e] = b4.x;
+                    b[e + 1] = b4.y;
+                    b[e + 2] = b4.z;
+                    b[e + 3] = b4.w;
                   }
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) b[e] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const float y = fmaf(x[e], sc, b[e]);
+                  x[e] = b[e] == -INFINITY || q * 16 + e >= keys ? -INFINITY : y;  // (whatever the row holds)
                 }
               }
               if (k < 2 * chunks) {
@@ -575,7 +597,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
                 uint32_t w[8];
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
-                  const float y0 = ex2_approx(x[e] + neg), y1 = ex2_approx(x[e + 1] + neg);
+                  const float y0 = ex2_approx(fmaf(x[e], to2, neg)), y1 = ex2_approx(fmaf(x[e + 1], to2, neg));
                   sum += y0 + y1;
                   w[e / 2] = pack_bf16(y0, y1);
                 }
@@ -605,13 +627,14 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
       tc_fence_after();
       if (warp_on) {
         float f[2] = {1.f, 1.f};
+        ref *= to2;  // (as it was used)
         if (MT == 1) {  // the row's sum in both chains
           sum_s[c * 128 + rl] = make_float2(ref, sum);
           named_bar_sync(pair_bar, 64);
           const float2 s0 = sum_s[rl], s1 = sum_s[128 + rl];
-          const float top = fmaxf(s0.x, s1.x), zero = top == -INFINITY ? 0.f : top;
-          f[0] = ex2_approx(s0.x - zero);
-          f[1] = ex2_approx(s1.x - zero);
+          const float top = fmaxf(s0.x, s1.x);  // (a number: the first chain has a tile)
+          f[0] = ex2_approx(s0.x - top);
+          f[1] = ex2_approx(s1.x - top);
           sum = s0.y * f[0] + s1.y * f[1];
           ref = top;
         }

@@ -146,6 +146,8 @@ class Case:
             bs[:] = -np.inf
         if bias == "lowest":
             bs[rng.random((B, hkv, cap)) < 0.5] = LOWEST
+        if bias == "all_lowest":
+            bs[:] = LOWEST
         bs = bs.astype(np.float32)
         for b in range(B):
             K[b, :, lengths[b]:] = V[b, :, lengths[b]:] = np.nan
@@ -216,7 +218,7 @@ ATTN = [
 
 @pytest.mark.parametrize("args", ATTN, ids=lambda a: "-".join(str(x).replace(" ", "") for x in a))
 @pytest.mark.parametrize("bias,parents", [("ratio", "tree"), (None, "chain"), ("masked", "forest"), ("none_left", "tree"),
-                                          ("lowest", "chain")])
+                                          ("lowest", "chain"), ("all_lowest", "forest")])
 def test_tree_attn(args, bias, parents):
     c = Case(*args, bias=bias, parents=parents)
     before = torch.full_like(c.q, 7.0)
