@@ -7,7 +7,9 @@
 //
 // Weights are held in 64-bit fixed point, units of 2^-62: an fp32 probability above 2^-39 is exact, differences and
 // sums are exact in any order, and so the token that a given number draws does not depend on how the vocabulary is
-// split.  (Sums in fp32 would move the borders between tokens by 2^-24 of the whole: one draw in a hundred
+// split.  After k rejections the weights are max(p - A q, 0) with A the sum of the masses that they were taken with
+// (max(max(x, 0) - y, 0) is max(x - y, 0) for y >= 0), so a pass costs the same however many there were.
+// (Sums in fp32 would move the borders between tokens by 2^-24 of the whole: one draw in a hundred
 // over a flat vocabulary of 128k.)
 #include "tree.cuh"
 
@@ -16,25 +18,35 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kSpan = 1024;             // entries of a warp's step: a sum is kept for each
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kSpan = 256;              // entries of a warp's step: a sum is kept for each
 constexpr int kMaxVocab = 1 << 20;
 constexpr u64 kOne = 1ull << 62;
 
 // a * b in units of 2^-62, for a < 2^64 and b < 2^62.
 __device__ __forceinline__ u64 mul_fix(u64 a, u64 b) { return (__umul64hi(a, b) << 2) | ((a * b) >> 62); }
+// A q in units of 2^-62, for A in units of 2^-kTimes below 2^(64 - kTimes) and q < 2^63; all ones where it is 4 or more (no weight
+// is left there: p < 2).
+constexpr int kTimes = 56;
+__device__ __forceinline__ u64 times_fix(u64 A, u64 q) {
+  const u64 hi = __umul64hi(A, q), lo = A * q;
+  return hi >> kTimes != 0 ? ~0ull : (hi << (64 - kTimes)) | (lo >> kTimes);
+}
 // A probability in fixed point; one that is none counts as 0.
 __device__ __forceinline__ u64 to_fix(float p, bool& bad) {
   const bool ok = p >= 0.f && p < 2.f;
   bad = bad || !ok;
-  return __float2ull_rz((ok ? p : 0.f) * 0x1p62f);
+  // the mantissa in its place, by shifts (the conversion instruction runs at a quarter of their rate)
+  const uint32_t u = ok ? __float_as_uint(p) : 0u;
+  const int shift = (int)(u >> 23) - 88;
+  const u64 m = (u & 0x7fffffu) | 0x800000u;
+  return shift >= 0 ? m << shift : shift > -32 ? (u64)((uint32_t)m >> -shift) : 0ull;
 }
 
 struct Smem {
   u64 span[kMaxVocab / kSpan + 1];  // sums of the CTA's spans
   u64 pt[SELKV_MAX_TREE];           // target probability of token t at its parent
   u64 qt[SELKV_MAX_TREE];           // draft's
-  u64 mult[SELKV_MAX_TREE];         // masses that the node's rejections were taken with
   u64 warp[kWarps];
   u64 part[2];                      // the CTA's sum, read by the cluster
   float u[SELKV_MAX_TREE];
@@ -62,66 +74,86 @@ struct Weights {
   const float* q;
   const Smem* sm;
   int rejected;
+  u64 A;     // sum of the masses that the rejections were taken with, units of 2^-kTimes
   bool vec;  // rows 16-byte aligned
 
-  __device__ __forceinline__ void load4x(const float* row, int i, int hi, float (&x)[4]) const {
-    if (vec && i + 3 < hi) {
-      const float4 v = *reinterpret_cast<const float4*>(row + i);
-      x[0] = v.x;
-      x[1] = v.y;
-      x[2] = v.z;
-      x[3] = v.w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = i + e < hi ? row[i + e] : 0.f;
-    }
+  __device__ __forceinline__ static float4 four(const float* row, int i, int hi, bool whole) {
+    if (whole) return *reinterpret_cast<const float4*>(row + i);
+    return make_float4(i < hi ? row[i] : 0.f, i + 1 < hi ? row[i + 1] : 0.f, i + 2 < hi ? row[i + 2] : 0.f, i + 3 < hi ? row[i + 3] : 0.f);
   }
-  __device__ __forceinline__ void of(int i, int hi, u64 (&r)[4], bool& bad) const {
-    float x[4], y[4];
-    load4x(p, i, hi, x);
-    if (DRAWN && rejected > 0) load4x(q, i, hi, y);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      r[e] = to_fix(x[e], bad);
-      if (DRAWN) {
-        if (rejected > 0) {
-          const u64 f = to_fix(y[e], bad);
-          for (int j = 0; j < rejected; ++j) {
-            const u64 m = j == 0 ? f : mul_fix(sm->mult[j], f);  // (the first mass is 1)
-            r[e] = r[e] > m ? r[e] - m : 0;
-          }
-        }
-      } else {
-        for (int j = 0; j < rejected; ++j)
-          if (sm->out[j] == i + e) r[e] = 0;
-      }
+  __device__ __forceinline__ bool uses_q() const { return DRAWN && rejected > 0; }
+  __device__ __forceinline__ u64 weight(float x, float y, bool& bad) const {
+    u64 r = to_fix(x, bad);
+    if (DRAWN && rejected > 0) {
+      const u64 f = to_fix(y, bad), m = rejected == 1 ? f : times_fix(A, f);  // (the first mass is 1)
+      r = r > m ? r - m : 0;
     }
+    return r;
+  }
+  // Entries i .. i + 3 from their probabilities; `taken`: some token near is taken out.
+  __device__ __forceinline__ void of(float4 x, float4 y, int i, bool taken, u64 (&r)[4], bool& bad) const {
+    r[0] = weight(x.x, y.x, bad);
+    r[1] = weight(x.y, y.y, bad);
+    r[2] = weight(x.z, y.z, bad);
+    r[3] = weight(x.w, y.w, bad);
+    if (!DRAWN && taken)
+      for (int j = 0; j < rejected; ++j) {
+        const int o = sm->out[j] - i;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (o == e) r[e] = 0;
+      }
+  }
+  // Whether a token between s0 and s0 + kSpan is taken out (the warp's).
+  __device__ __forceinline__ bool takes(int s0) const {
+    bool t = false;
+    if (!DRAWN)
+      for (int j = threadIdx.x & 31; j < rejected; j += 32) t = t || (sm->out[j] >= s0 && sm->out[j] < s0 + kSpan);
+    return !DRAWN && rejected > 0 && __any_sync(0xffffffffu, t);
   }
 };
 
 // The sum of the weights over the vocabulary: this CTA's entries lo .. hi - 1 span by span, then the cluster's CTAs.
+// Two spans' loads are on their way together.
 template <bool DRAWN>
 __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, int ctas, int& phase, bool& bad) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int kRows = kSpan / 128;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, spans = (hi - lo + kSpan - 1) / kSpan;
   u64 mine = 0;
-  for (int s0 = lo + warp * kSpan, s = warp; s0 < hi; s0 += kWarps * kSpan, s += kWarps) {
-    u64 sum = 0;
+  for (int s = warp; s < spans; s += 2 * kWarps) {
+    float4 x[2][kRows], y[2][kRows];
 #pragma unroll
-    for (int k = 0; k < kSpan / 128; ++k) {
-      u64 r[4];
-      w.of(s0 + k * 128 + lane * 4, hi, r, bad);
-      sum += (r[0] + r[1]) + (r[2] + r[3]);
+    for (int h = 0; h < 2; ++h) {
+      const int s0 = lo + (s + h * kWarps) * kSpan;
+      const bool whole = w.vec && s0 + kSpan <= hi;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        x[h][k] = Weights<DRAWN>::four(w.p, s0 + k * 128 + lane * 4, hi, whole);
+        y[h][k] = w.uses_q() ? Weights<DRAWN>::four(w.q, s0 + k * 128 + lane * 4, hi, whole) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
     }
-    sum = warp_sum_u64(sum);
-    if (lane == 0) sm->span[s] = sum;
-    mine += sum;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = s + h * kWarps;
+      if (at >= spans) continue;
+      const bool taken = w.takes(lo + at * kSpan);
+      u64 sum = 0;
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        u64 r[4];
+        w.of(x[h][k], y[h][k], lo + at * kSpan + k * 128 + lane * 4, taken, r, bad);
+        sum += (r[0] + r[1]) + (r[2] + r[3]);
+      }
+      sum = warp_sum_u64(sum);
+      if (lane == 0) sm->span[at] = sum;
+      mine += sum;
+    }
   }
   if (lane == 0) sm->warp[warp] = mine;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    u64 t = 0;
-    for (int i = 0; i < kWarps; ++i) t += sm->warp[i];
-    sm->part[phase & 1] = t;
+  if (threadIdx.x < 32) {
+    const u64 t = warp_sum_u64(threadIdx.x < kWarps ? sm->warp[threadIdx.x] : 0);
+    if (threadIdx.x == 0) sm->part[phase & 1] = t;
   }
   cluster_arrive();
   cluster_wait();
@@ -147,28 +179,28 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
   }
   const float* target = a.target + (size_t)b * a.T * a.V;
   const float* draft = DRAWN ? a.draft + (size_t)b * a.T * a.V : nullptr;
-  if (tid < n) {
-    int p = -1;
-    if (tid > 0) {
-      p = a.parents != nullptr ? a.parents[(size_t)b * a.T + tid] : tid - 1;
-      if (p < -1 || p >= tid) {
-        flags |= SELKV_DEVERR_TREE;
-        p = -1;
-      }
-    }
+  if (tid < a.T) {
+    // (what the count does not decide is asked for beside it)
+    int p = tid > 0 ? (a.parents != nullptr ? a.parents[(size_t)b * a.T + tid] : tid - 1) : -1;
     float u = a.uniforms[(size_t)b * a.T + tid];
-    if (!(u >= 0.f && u < 1.f)) {
-      bad = true;
-      u = u >= 1.f ? 0x1.fffffep-1f : 0.f;
-    }
     const int x = tid > 0 ? a.tokens[(size_t)b * a.T + tid] : 0;
     u64 pt = 0, qt = kOne;
-    if (p >= 0) {
-      if (x >= 0 && x < a.V) {
-        pt = to_fix(target[(size_t)p * a.V + x], bad);
-        if (DRAWN) qt = to_fix(draft[(size_t)p * a.V + x], bad);
-      } else {
+    if (tid < n) {
+      if (p < -1 || p >= tid) {
+        if (tid > 0) flags |= SELKV_DEVERR_TREE;
+        p = -1;
+      }
+      if (!(u >= 0.f && u < 1.f)) {
         bad = true;
+        u = u >= 1.f ? 0x1.fffffep-1f : 0.f;
+      }
+      if (p >= 0) {
+        if (x >= 0 && x < a.V) {
+          pt = to_fix(target[(size_t)p * a.V + x], bad);
+          if (DRAWN) qt = to_fix(draft[(size_t)p * a.V + x], bad);
+        } else {
+          bad = true;
+        }
       }
     }
     sm->parent[tid] = p;
@@ -177,20 +209,18 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
     sm->pt[tid] = pt;
     sm->qt[tid] = qt;
   }
-  if (tid == 0) {
-    sm->mult[0] = kOne;
-    // (the token of rows without mass; another CTA's draw comes behind the cluster's first barrier)
-    if (rank == 0) a.next[b] = n > 0 ? a.V - 1 : -1;
-  }
+  // (the token of rows without mass; another CTA's draw comes behind the cluster's first barrier)
+  if (tid == 0 && rank == 0) a.next[b] = n > 0 ? a.V - 1 : -1;
   __syncthreads();
 
   // The walk; every thread of the cluster takes the same way.
   int node = 0, taken = n > 0 ? 1 : 0, rejected = 0, phase = 0;
   u64 M = kOne, Z = 0;  // the mass of the tests, and the sum over the vocabulary where it is known
+  u64 A = 0;            // the sum of the masses that the node's rejections were taken with
   bool known = false;
   const bool vec = (a.V & 3) == 0;
-  auto weights = [&](int rej) {
-    return Weights<DRAWN>{target + (size_t)node * a.V, DRAWN ? draft + (size_t)node * a.V : nullptr, sm, rej, vec};
+  auto weights = [&](int rej, u64 times) {
+    return Weights<DRAWN>{target + (size_t)node * a.V, DRAWN ? draft + (size_t)node * a.V : nullptr, sm, rej, times, vec};
   };
   if (tid == 0) sm->path[0] = 0;
   for (int t = 1; t < n; ++t) {
@@ -200,8 +230,8 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
     u64 r = sm->pt[t];
     const int x = sm->token[t];
     if (DRAWN) {
-      for (int j = 0; j < rejected; ++j) {
-        const u64 m = mul_fix(sm->mult[j], sm->qt[t]);
+      if (rejected > 0) {
+        const u64 m = rejected == 1 ? sm->qt[t] : times_fix(A, sm->qt[t]);
         r = r > m ? r - m : 0;
       }
     } else {
@@ -214,17 +244,19 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
       node = t;
       rejected = 0;
       M = kOne;
+      A = 0;
       known = false;
       continue;
     }
     // a rejection: the weights that are left, and their mass
     if (DRAWN) {
-      const u64 left = sum_weights(weights(rejected + 1), sm, lo, hi, ctas, phase, bad);
+      const u64 more = A + (M >> (62 - kTimes));
+      const u64 left = sum_weights(weights(rejected + 1, more), sm, lo, hi, ctas, phase, bad);
       known = left > 0;
       if (known) {
         Z = M = left;
+        A = more;
         ++rejected;
-        if (rejected < SELKV_MAX_TREE && tid == 0) sm->mult[rejected] = left;
       }
     } else if (M > r) {
       M -= r;
@@ -234,7 +266,7 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
     __syncthreads();
   }
   if (n > 0) {
-    if (!known) Z = sum_weights(weights(rejected), sm, lo, hi, ctas, phase, bad);
+    if (!known) Z = sum_weights(weights(rejected, A), sm, lo, hi, ctas, phase, bad);
     // the CTA and the span that the number falls into, then the entry
     bool bu = false;
     const u64 at = mul_fix(Z, to_fix(sm->u[0], bu));
@@ -243,6 +275,9 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
       below += own;
       own = ld_peer_u64(peer_smem(smem_u32(&sm->part[(phase - 1) & 1]), c));
     }
+    // (no CTA leaves or goes on while another reads its sum; from here on they need one another no more)
+    cluster_arrive();
+    cluster_wait();
     if (Z == 0) bad = true;
     else if (tid < 32 && at >= below && at - below < own) {
       const int spans = (hi - lo + kSpan - 1) / kSpan;
@@ -266,11 +301,15 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
         }
         rest -= inck;
       }
-      const Weights<DRAWN> w = weights(rejected);
+      const Weights<DRAWN> w = weights(rejected, A);
+      const int s0 = lo + s * kSpan;
+      const bool whole = vec && s0 + kSpan <= hi, taken = w.takes(s0);
+#pragma unroll 1
       for (int k = 0; k < kSpan / 128; ++k) {
-        const int i = lo + s * kSpan + k * 128 + tid * 4;
+        const int i = s0 + k * 128 + tid * 4;
         u64 r[4];
-        w.of(i, hi, r, bad);
+        w.of(Weights<DRAWN>::four(w.p, i, hi, whole), w.uses_q() ? Weights<DRAWN>::four(w.q, i, hi, whole) : make_float4(0.f, 0.f, 0.f, 0.f), i,
+             taken, r, bad);
         const u64 v = (r[0] + r[1]) + (r[2] + r[3]);
         u64 inc = v;
 #pragma unroll
@@ -292,16 +331,13 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
       }
     }
   }
-  __syncthreads();
   if (rank == 0) {
+    __syncthreads();  // the path is written
     if (tid < a.T) a.path[(size_t)b * a.T + tid] = tid < taken ? sm->path[tid] : -1;
     if (tid == 0) a.accepted[b] = taken;
   }
   if (bad) flags |= SELKV_DEVERR_VALUE;
   if (flags != 0) raise_flag(a.flags, flags);
-  // no CTA leaves while another reads its sum
-  cluster_arrive();
-  cluster_wait();
 }
 
 template <bool DRAWN>
