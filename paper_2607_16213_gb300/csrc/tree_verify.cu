@@ -5,12 +5,13 @@
 // start, and a cluster of CTAs holds a part of the vocabulary each, so the walk costs a memory round trip and a
 // pass for each rejection; the passes read the distributions of the nodes they are at and no others.
 //
-// Weights are held in 64-bit fixed point, units of 2^-62: an fp32 probability above 2^-39 is exact, differences and
-// sums are exact in any order, and so the token that a given number draws does not depend on how the vocabulary is
-// split.  After k rejections the weights are max(p - A q, 0) with A the sum of the masses that they were taken with
-// (max(max(x, 0) - y, 0) is max(x - y, 0) for y >= 0), so a pass costs the same however many there were.
-// (Sums in fp32 would move the borders between tokens by 2^-24 of the whole: one draw in a hundred
-// over a flat vocabulary of 128k.)
+// Tests and sums are held in 64-bit fixed point, units of 2^-62.  A pass adds up each thread's few weights as an fp32 number and its
+// error (an exact difference of three operations and an exact sum of six, where a 64-bit sum took 70 instructions an entry)
+// and goes on in fixed point from there: 47 bits or more.  So the token that a given number draws does not depend on
+// how the vocabulary is split, but for borders within 2^-47 of it.  (Sums in fp32 would move the borders between tokens by
+// 2^-24 of the whole: one draw in a hundred over a flat vocabulary of 128k.)  After k rejections the weights are
+// max(p - A q, 0) with A the sum of the masses that they were taken with (max(max(x, 0) - y, 0) is max(x - y, 0) for
+// y >= 0), so a pass costs the same however many there were.
 #include "tree.cuh"
 
 namespace selkv {
@@ -67,6 +68,17 @@ __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
   return v;
 }
 
+// A sum of fp32 numbers as the rounded sum and what it is short of.
+struct Pair {
+  float s, e;
+  __device__ __forceinline__ void add(float x, float more) {
+    const float t = s + x, b = t - s;
+    e += (s - (t - b)) + (x - b) + more;
+    s = t;
+  }
+  __device__ __forceinline__ u64 fixed() const { return __float2ull_rz(s * 0x1p62f) + (u64)__float2ll_rn(e * 0x1p62f); }
+};
+
 // The vocabulary's entries at one node, after the node's rejections.
 template <bool DRAWN>
 struct Weights {
@@ -74,15 +86,28 @@ struct Weights {
   const float* q;
   const Smem* sm;
   int rejected;
-  u64 A;     // sum of the masses that the rejections were taken with, units of 2^-kTimes
-  bool vec;  // rows 16-byte aligned
+  u64 A;         // sum of the masses that the rejections were taken with, units of 2^-kTimes
+  float Ah, Al;  // the same as an fp32 number and the rest
+  bool vec;      // rows 16-byte aligned
 
   __device__ __forceinline__ static float4 four(const float* row, int i, int hi, bool whole) {
     if (whole) return *reinterpret_cast<const float4*>(row + i);
     return make_float4(i < hi ? row[i] : 0.f, i + 1 < hi ? row[i + 1] : 0.f, i + 2 < hi ? row[i + 2] : 0.f, i + 3 < hi ? row[i + 3] : 0.f);
   }
   __device__ __forceinline__ bool uses_q() const { return DRAWN && rejected > 0; }
-  __device__ __forceinline__ u64 weight(float x, float y, bool& bad) const {
+  // What is no probability counts as 0.
+  __device__ __forceinline__ static void clean(float4& v, bool& bad) {
+    if (((__float_as_uint(v.x) | __float_as_uint(v.y) | __float_as_uint(v.z) | __float_as_uint(v.w)) >> 30) == 0u) return;
+    float* x = reinterpret_cast<float*>(&v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool ok = x[e] >= 0.f && x[e] < 2.f;
+      bad = bad || !ok;
+      x[e] = ok ? x[e] : 0.f;
+    }
+  }
+  __device__ __forceinline__ u64 weight(float x, float y) const {
+    bool bad = false;
     u64 r = to_fix(x, bad);
     if (DRAWN && rejected > 0) {
       const u64 f = to_fix(y, bad), m = rejected == 1 ? f : times_fix(A, f);  // (the first mass is 1)
@@ -90,19 +115,25 @@ struct Weights {
     }
     return r;
   }
-  // Entries i .. i + 3 from their probabilities; `taken`: some token near is taken out.
-  __device__ __forceinline__ void of(float4 x, float4 y, int i, bool taken, u64 (&r)[4], bool& bad) const {
-    r[0] = weight(x.x, y.x, bad);
-    r[1] = weight(x.y, y.y, bad);
-    r[2] = weight(x.z, y.z, bad);
-    r[3] = weight(x.w, y.w, bad);
-    if (!DRAWN && taken)
-      for (int j = 0; j < rejected; ++j) {
-        const int o = sm->out[j] - i;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (o == e) r[e] = 0;
-      }
+  __device__ __forceinline__ bool is_out(int i) const {
+    for (int j = 0; j < rejected; ++j)
+      if (sm->out[j] == i) return true;
+    return false;
+  }
+  // The weight of one entry onto a sum.
+  __device__ __forceinline__ void onto(Pair& sum, float x, float y) const {
+    if (!DRAWN || rejected == 0) {
+      sum.add(x, 0.f);
+    } else if (rejected == 1) {
+      const float s = x - y, e = (x - s) - y;  // exact for x > y >= 0
+      const bool pos = x > y;
+      sum.add(pos ? s : 0.f, pos ? e : 0.f);
+    } else {
+      const float h = __fmul_rn(Ah, y), l = fmaf(Ah, y, -h) + Al * y;
+      const float s = x - h, b = s - x, e = ((x - (s - b)) - (h + b)) - l;
+      const bool pos = s + e > 0.f;
+      sum.add(pos ? s : 0.f, pos ? e : 0.f);
+    }
   }
   // Whether a token between s0 and s0 + kSpan is taken out (the warp's).
   __device__ __forceinline__ bool takes(int s0) const {
@@ -137,16 +168,27 @@ __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, in
       const int at = s + h * kWarps;
       if (at >= spans) continue;
       const bool taken = w.takes(lo + at * kSpan);
-      u64 sum = 0;
+      Pair sum{0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        u64 r[4];
-        w.of(x[h][k], y[h][k], lo + at * kSpan + k * 128 + lane * 4, taken, r, bad);
-        sum += (r[0] + r[1]) + (r[2] + r[3]);
+        float4 a = x[h][k], c = y[h][k];
+        Weights<DRAWN>::clean(a, bad);
+        if (DRAWN) Weights<DRAWN>::clean(c, bad);
+        if (taken) {
+          const int i = lo + at * kSpan + k * 128 + lane * 4;
+          a.x = w.is_out(i) ? 0.f : a.x;
+          a.y = w.is_out(i + 1) ? 0.f : a.y;
+          a.z = w.is_out(i + 2) ? 0.f : a.z;
+          a.w = w.is_out(i + 3) ? 0.f : a.w;
+        }
+        w.onto(sum, a.x, c.x);
+        w.onto(sum, a.y, c.y);
+        w.onto(sum, a.z, c.z);
+        w.onto(sum, a.w, c.w);
       }
-      sum = warp_sum_u64(sum);
-      if (lane == 0) sm->span[at] = sum;
-      mine += sum;
+      const u64 f = warp_sum_u64(sum.fixed());
+      if (lane == 0) sm->span[at] = f;
+      mine += f;
     }
   }
   if (lane == 0) sm->warp[warp] = mine;
@@ -220,7 +262,9 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
   bool known = false;
   const bool vec = (a.V & 3) == 0;
   auto weights = [&](int rej, u64 times) {
-    return Weights<DRAWN>{target + (size_t)node * a.V, DRAWN ? draft + (size_t)node * a.V : nullptr, sm, rej, times, vec};
+    const float high = __ull2float_rn(times) * 0x1p-56f;
+    const float low = __ll2float_rn((long long)(times - __float2ull_rz(high * 0x1p56f))) * 0x1p-56f;
+    return Weights<DRAWN>{target + (size_t)node * a.V, DRAWN ? draft + (size_t)node * a.V : nullptr, sm, rej, times, high, low, vec};
   };
   if (tid == 0) sm->path[0] = 0;
   for (int t = 1; t < n; ++t) {
@@ -307,9 +351,15 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
 #pragma unroll 1
       for (int k = 0; k < kSpan / 128; ++k) {
         const int i = s0 + k * 128 + tid * 4;
-        u64 r[4];
-        w.of(Weights<DRAWN>::four(w.p, i, hi, whole), w.uses_q() ? Weights<DRAWN>::four(w.q, i, hi, whole) : make_float4(0.f, 0.f, 0.f, 0.f), i,
-             taken, r, bad);
+        float4 x = Weights<DRAWN>::four(w.p, i, hi, whole);
+        float4 y = w.uses_q() ? Weights<DRAWN>::four(w.q, i, hi, whole) : make_float4(0.f, 0.f, 0.f, 0.f);
+        Weights<DRAWN>::clean(x, bad);
+        Weights<DRAWN>::clean(y, bad);
+        u64 r[4] = {w.weight(x.x, y.x), w.weight(x.y, y.y), w.weight(x.z, y.z), w.weight(x.w, y.w)};
+        if (taken) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r[e] = w.is_out(i + e) ? 0 : r[e];
+        }
         const u64 v = (r[0] + r[1]) + (r[2] + r[3]);
         u64 inc = v;
 #pragma unroll
@@ -328,6 +378,10 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
           break;
         }
         rest -= __shfl_sync(0xffffffffu, inc, 31);
+        // (the entries' sum may fall short of the span's by its rounding: then the last one that has weight)
+        const uint32_t some = __ballot_sync(0xffffffffu, v > 0);
+        if (some != 0 && tid == 31 - __clz(some)) a.next[b] = min(i + (r[3] > 0 ? 3 : r[2] > 0 ? 2 : r[1] > 0 ? 1 : 0), a.V - 1);
+        __syncwarp();
       }
     }
   }
