@@ -52,9 +52,13 @@ struct Smem {
   u64 part[2];                      // the CTA's sum, read by the cluster
   float u[SELKV_MAX_TREE];
   int parent[SELKV_MAX_TREE];
+  uint32_t first[SELKV_MAX_TREE / 32];  // tokens that are accepted when no child of their parent was rejected before, as bits
   int token[SELKV_MAX_TREE];
   int out[SELKV_MAX_TREE];          // tokens taken out at the node (picked drafts)
   int path[SELKV_MAX_TREE];
+  // where the walk stands, from the warp that takes it to the others
+  int node, rejected, taken, more;  // more: it goes on behind the pass
+  u64 A;
 };
 
 __device__ __forceinline__ u64 ld_peer_u64(uint32_t peer) {
@@ -120,14 +124,14 @@ struct Weights {
       if (sm->out[j] == i) return true;
     return false;
   }
-  // The weight of one entry onto a sum.
+  // The weight of one entry onto a sum, after no (kAfter 0), one or more rejections of drawn drafts.
+  template <int kAfter>
   __device__ __forceinline__ void onto(Pair& sum, float x, float y) const {
-    if (!DRAWN || rejected == 0) {
+    if (kAfter == 0) {
       sum.add(x, 0.f);
-    } else if (rejected == 1) {
-      const float s = x - y, e = (x - s) - y;  // exact for x > y >= 0
-      const bool pos = x > y;
-      sum.add(pos ? s : 0.f, pos ? e : 0.f);
+    } else if (kAfter == 1) {
+      const float z = fmaxf(x, y), s = z - y, e = (z - s) - y;  // exact for x > y >= 0, and 0 for the others
+      sum.add(s, e);
     } else {
       const float h = __fmul_rn(Ah, y), l = fmaf(Ah, y, -h) + Al * y;
       const float s = x - h, b = s - x, e = ((x - (s - b)) - (h + b)) - l;
@@ -144,23 +148,33 @@ struct Weights {
   }
 };
 
-// The sum of the weights over the vocabulary: this CTA's entries lo .. hi - 1 span by span, then the cluster's CTAs.
-// Two spans' loads are on their way together.
-template <bool DRAWN>
-__device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, int ctas, int& phase, bool& bad) {
+// This warp's part of the sum of the weights over the CTA's entries lo .. hi - 1, span by span; two spans' loads are on
+// their way together.
+template <bool DRAWN, int kAfter>
+__device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, bool& bad) {
   constexpr int kRows = kSpan / 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, spans = (hi - lo + kSpan - 1) / kSpan;
   u64 mine = 0;
+#pragma unroll 1
   for (int s = warp; s < spans; s += 2 * kWarps) {
     float4 x[2][kRows], y[2][kRows];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int s0 = lo + (s + h * kWarps) * kSpan;
-      const bool whole = w.vec && s0 + kSpan <= hi;
+      if (w.vec && s0 + kSpan <= hi) {
+        const float4* p = reinterpret_cast<const float4*>(w.p + s0) + lane;
+        const float4* q = reinterpret_cast<const float4*>(w.q + s0) + lane;
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) {
-        x[h][k] = Weights<DRAWN>::four(w.p, s0 + k * 128 + lane * 4, hi, whole);
-        y[h][k] = w.uses_q() ? Weights<DRAWN>::four(w.q, s0 + k * 128 + lane * 4, hi, whole) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < kRows; ++k) {
+          x[h][k] = p[k * 32];
+          if (kAfter > 0) y[h][k] = q[k * 32];
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+          x[h][k] = Weights<DRAWN>::four(w.p, s0 + k * 128 + lane * 4, hi, false);
+          if (kAfter > 0) y[h][k] = Weights<DRAWN>::four(w.q, s0 + k * 128 + lane * 4, hi, false);
+        }
       }
     }
 #pragma unroll
@@ -171,9 +185,9 @@ __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, in
       Pair sum{0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < kRows; ++k) {
-        float4 a = x[h][k], c = y[h][k];
+        float4 a = x[h][k], c = kAfter > 0 ? y[h][k] : make_float4(0.f, 0.f, 0.f, 0.f);
         Weights<DRAWN>::clean(a, bad);
-        if (DRAWN) Weights<DRAWN>::clean(c, bad);
+        if (kAfter > 0) Weights<DRAWN>::clean(c, bad);
         if (taken) {
           const int i = lo + at * kSpan + k * 128 + lane * 4;
           a.x = w.is_out(i) ? 0.f : a.x;
@@ -181,16 +195,27 @@ __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, in
           a.z = w.is_out(i + 2) ? 0.f : a.z;
           a.w = w.is_out(i + 3) ? 0.f : a.w;
         }
-        w.onto(sum, a.x, c.x);
-        w.onto(sum, a.y, c.y);
-        w.onto(sum, a.z, c.z);
-        w.onto(sum, a.w, c.w);
+        w.template onto<kAfter>(sum, a.x, c.x);
+        w.template onto<kAfter>(sum, a.y, c.y);
+        w.template onto<kAfter>(sum, a.z, c.z);
+        w.template onto<kAfter>(sum, a.w, c.w);
       }
       const u64 f = warp_sum_u64(sum.fixed());
       if (lane == 0) sm->span[at] = f;
       mine += f;
     }
   }
+  return mine;
+}
+
+// The sum of the weights over the vocabulary: this CTA's entries, then the cluster's CTAs.
+template <bool DRAWN>
+__device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, int ctas, int& phase, bool& bad) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  u64 mine;
+  if (!DRAWN || w.rejected == 0) mine = sum_spans<DRAWN, 0>(w, sm, lo, hi, bad);
+  else if (w.rejected == 1) mine = sum_spans<DRAWN, 1>(w, sm, lo, hi, bad);
+  else mine = sum_spans<DRAWN, 2>(w, sm, lo, hi, bad);
   if (lane == 0) sm->warp[warp] = mine;
   __syncthreads();
   if (threadIdx.x < 32) {
@@ -221,6 +246,7 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
   }
   const float* target = a.target + (size_t)b * a.T * a.V;
   const float* draft = DRAWN ? a.draft + (size_t)b * a.T * a.V : nullptr;
+  bool yes = false;
   if (tid < a.T) {
     // (what the count does not decide is asked for beside it)
     int p = tid > 0 ? (a.parents != nullptr ? a.parents[(size_t)b * a.T + tid] : tid - 1) : -1;
@@ -250,67 +276,127 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
     sm->u[tid] = u;
     sm->pt[tid] = pt;
     sm->qt[tid] = qt;
+    bool none = false;
+    yes = mul_fix(to_fix(u, none), qt) < pt;
+  }
+  if (tid < SELKV_MAX_TREE) {
+    const uint32_t bits = __ballot_sync(0xffffffffu, yes);
+    if ((tid & 31) == 0) sm->first[tid >> 5] = bits;
   }
   // (the token of rows without mass; another CTA's draw comes behind the cluster's first barrier)
   if (tid == 0 && rank == 0) a.next[b] = n > 0 ? a.V - 1 : -1;
   __syncthreads();
 
-  // The walk; every thread of the cluster takes the same way.
-  int node = 0, taken = n > 0 ? 1 : 0, rejected = 0, phase = 0;
-  u64 M = kOne, Z = 0;  // the mass of the tests, and the sum over the vocabulary where it is known
-  u64 A = 0;            // the sum of the masses that the node's rejections were taken with
-  bool known = false;
+  // The walk, by the first warp of each CTA of the cluster in the same way, from one pass over the vocabulary to the next.
+  // The others take part in the passes.
+  int phase = 0;
   const bool vec = (a.V & 3) == 0;
-  auto weights = [&](int rej, u64 times) {
+  auto weights = [&](int node, int rej, u64 times) {
     const float high = __ull2float_rn(times) * 0x1p-56f;
     const float low = __ll2float_rn((long long)(times - __float2ull_rz(high * 0x1p56f))) * 0x1p-56f;
     return Weights<DRAWN>{target + (size_t)node * a.V, DRAWN ? draft + (size_t)node * a.V : nullptr, sm, rej, times, high, low, vec};
   };
-  if (tid == 0) sm->path[0] = 0;
-  for (int t = 1; t < n; ++t) {
-    if (sm->parent[t] != node) continue;
-    bool bu = false;
-    const u64 u = to_fix(sm->u[t], bu);
-    u64 r = sm->pt[t];
-    const int x = sm->token[t];
-    if (DRAWN) {
-      if (rejected > 0) {
-        const u64 m = rejected == 1 ? sm->qt[t] : times_fix(A, sm->qt[t]);
-        r = r > m ? r - m : 0;
-      }
-    } else {
-      for (int j = 0; j < rejected; ++j)
-        if (sm->out[j] == x) r = 0;
-    }
-    if (mul_fix(u, DRAWN ? mul_fix(M, sm->qt[t]) : M) < r) {
-      if (tid == 0) sm->path[taken] = t;
-      ++taken;
-      node = t;
-      rejected = 0;
-      M = kOne;
-      A = 0;
-      known = false;
-      continue;
-    }
-    // a rejection: the weights that are left, and their mass
-    if (DRAWN) {
-      const u64 more = A + (M >> (62 - kTimes));
-      const u64 left = sum_weights(weights(rejected + 1, more), sm, lo, hi, ctas, phase, bad);
-      known = left > 0;
-      if (known) {
-        Z = M = left;
-        A = more;
-        ++rejected;
-      }
-    } else if (M > r) {
-      M -= r;
-      if (tid == 0) sm->out[rejected] = x;
-      ++rejected;
-    }
-    __syncthreads();
-  }
+  int node = 0, taken = n > 0 ? 1 : 0, rejected = 0;
+  u64 M = kOne, Z = 0;  // the mass of the tests, and the sum over the vocabulary where it is known
+  u64 A = 0;            // the sum of the masses that the node's rejections were taken with
   if (n > 0) {
-    if (!known) Z = sum_weights(weights(rejected, A), sm, lo, hi, ctas, phase, bad);
+    uint32_t kids[SELKV_MAX_TREE / 32];  // the node's children that are not tried yet, as bits
+    auto children = [&] {
+#pragma unroll
+      for (int k = 0; k < SELKV_MAX_TREE / 32; ++k) {
+        kids[k] = 0u;
+        if (k * 32 >= n) continue;
+        const int t = k * 32 + (tid & 31);
+        kids[k] = __ballot_sync(0xffffffffu, t > node && t < n && sm->parent[t] == node);
+      }
+    };
+    if (tid < 32) {
+      children();
+      if (tid == 0) sm->path[0] = 0;
+    }
+    bool known = false;  // Z is the sum of the weights as they are
+    for (;;) {
+      if (tid < 32) {
+        bool pass = false;
+        for (;;) {
+          int t = -1;
+#pragma unroll
+          for (int k = SELKV_MAX_TREE / 32 - 1; k >= 0; --k)
+            if (kids[k] != 0u) t = k * 32 + __ffs(kids[k]) - 1;
+          if (t < 0) break;
+#pragma unroll
+          for (int k = 0; k < SELKV_MAX_TREE / 32; ++k)
+            if (t >> 5 == k) kids[k] &= kids[k] - 1u;
+          bool accept;
+          u64 r = 0;
+          const int x = sm->token[t];
+          if (rejected == 0) {
+            accept = (sm->first[t >> 5] >> (t & 31)) & 1u;
+            if (!DRAWN && !accept) r = sm->pt[t];
+          } else {
+            bool none = false;
+            const u64 u = to_fix(sm->u[t], none);
+            r = sm->pt[t];
+            if (DRAWN) {
+              const u64 m = rejected == 1 ? sm->qt[t] : times_fix(A, sm->qt[t]);
+              r = r > m ? r - m : 0;
+            } else {
+              for (int j = 0; j < rejected; ++j)
+                if (sm->out[j] == x) r = 0;
+            }
+            accept = mul_fix(u, DRAWN ? mul_fix(M, sm->qt[t]) : M) < r;
+          }
+          if (accept) {
+            if (tid == 0) sm->path[taken] = t;
+            ++taken;
+            node = t;
+            rejected = 0;
+            M = kOne;
+            A = 0;
+            known = false;
+            children();
+            continue;
+          }
+          // a rejection: the weights that are left, and their mass
+          if (DRAWN) {
+            pass = true;
+            break;
+          }
+          if (M > r) {
+            M -= r;
+            if (tid == 0) sm->out[rejected] = x;
+            ++rejected;
+          }
+          __syncwarp();
+        }
+        if (tid == 0) {
+          sm->node = node;
+          sm->rejected = rejected + (pass ? 1 : 0);
+          sm->taken = taken;
+          sm->more = pass ? 1 : known ? -1 : 0;
+          sm->A = pass ? A + (M >> (62 - kTimes)) : A;
+        }
+      }
+      __syncthreads();
+      const int more = sm->more;
+      if (more < 0) break;
+      const u64 sum = sum_weights(weights(sm->node, sm->rejected, sm->A), sm, lo, hi, ctas, phase, bad);
+      if (more == 0) {
+        Z = sum;
+        break;
+      }
+      if (tid < 32) {
+        known = sum > 0;
+        if (known) {
+          Z = M = sum;
+          A = sm->A;
+          ++rejected;
+        }
+      }
+      // (sm's words are read: the cluster's barrier of the sum lies behind them)
+    }
+    node = sm->node;
+    taken = sm->taken;
     // the CTA and the span that the number falls into, then the entry
     bool bu = false;
     const u64 at = mul_fix(Z, to_fix(sm->u[0], bu));
@@ -322,7 +408,8 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
     // (no CTA leaves or goes on while another reads its sum; from here on they need one another no more)
     cluster_arrive();
     cluster_wait();
-    if (Z == 0) bad = true;
+    // (the first warp's from here on: it knows the sum)
+    if (tid < 32 && Z == 0) bad = true;
     else if (tid < 32 && at >= below && at - below < own) {
       const int spans = (hi - lo + kSpan - 1) / kSpan;
       u64 rest = at - below;  // mass before the entry
@@ -345,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int
         }
         rest -= inck;
       }
-      const Weights<DRAWN> w = weights(rejected, A);
+      const Weights<DRAWN> w = weights(node, rejected, A);
       const int s0 = lo + s * kSpan;
       const bool whole = vec && s0 + kSpan <= hi, taken = w.takes(s0);
 #pragma unroll 1
