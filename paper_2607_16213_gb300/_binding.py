@@ -163,9 +163,7 @@ def exported_symbols() -> list:
 
 
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
@@ -361,14 +359,15 @@ def selkv_tree_commit_workspace_size(shape: selkv_shape) -> int:
 
 def selkv_tree_commit(shape: selkv_shape, tokens: int, path, accepted, K_new, V_new, K_c, V_c, bias, lengths, workspace,
                       workspace_bytes: int, stream=None) -> int:
-    """K_new, V_new, K_c, V_c, lengths: sequences of per-layer tensors (or device addresses); bias too, or None,
-    or with entries None."""
+    """K_new, V_new, K_c, V_c, lengths: sequences of per-layer tensors (or device addresses, or ctypes arrays of
+    them); bias too, or None, or with entries None."""
     L = len(K_new)
     if not all(len(x) == L for x in (V_new, K_c, V_c, lengths)) or (bias is not None and len(bias) != L):
         return SELKV_ERR_INVALID_ARG
+    kind = c_vp * max(1, L)
 
     def table(x):
-        return (c_vp * max(1, L))(*[_ptr(t) for t in x])
+        return x if x is None or isinstance(x, kind) else kind(*map(_ptr, x))
     return library().selkv_tree_commit(ctypes.byref(shape), L, int(tokens), _ptr(path), _ptr(accepted), table(K_new),
-                                       table(V_new), table(K_c), table(V_c), table(bias) if bias is not None else None,
-                                       table(lengths), _ptr(workspace), int(workspace_bytes), _stream(stream))
+                                       table(V_new), table(K_c), table(V_c), table(bias), table(lengths),
+                                       _ptr(workspace), int(workspace_bytes), _stream(stream))

@@ -317,10 +317,46 @@ def rotary_plan(rot_dim: int, theta: float = 10000.0, layout: str = "half", scal
     return plan
 
 
+def _fit(shape, dtype, index: int, *tensors) -> bool:
+    """Whether all of `tensors` are contiguous, of that shape and type, on that device (`_tensor` says which is not)."""
+    for t in tensors:
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+            return False
+    return True
+
+
+def _look(what: str, c: CompressedCache, key: bytes, dt, dev) -> tuple:
+    """The addresses of the tensors of a cache with the shape whose bytes are `key`; they are looked over when they are
+    others than the last time: other tensors, other memory or another shape."""
+    s = c.shape
+    K, V, b, n = c.K_c, c.V_c, c.bias, c.lengths
+    now = (key, dev, K.data_ptr(), V.data_ptr(), b.data_ptr() if b is not None else None, n.data_ptr())
+    seen = c.__dict__.get("_seen")
+    if seen is None or seen[0] != now or seen[1] is not K or seen[2] is not V or seen[3] is not b or seen[4] is not n:
+        rows = (s.batch, s.num_kv_heads, s.m_cap)
+        _tensor(K, what + ": K_c", rows + (s.head_dim,), dt, dev)
+        _tensor(V, what + ": V_c", rows + (s.head_dim,), dt, dev)
+        _tensor(n, what + ": lengths", (s.batch,), torch.int32, dev)
+        if b is not None:
+            _tensor(b, what + ": bias", rows, torch.float32, dev)
+        c._seen = (now, K, V, b, n)
+    return now
+
+
 def _cuda(t: torch.Tensor, name: str) -> torch.device:
     if t.device.type != "cuda":
         _bad("%s: a tensor of a CUDA device" % name)
     return t.device
+
+
+def _rotary_pair(name: str, x: torch.Tensor, out: Optional[torch.Tensor], want, dt, dev) -> torch.Tensor:
+    if out is None:
+        _tensor(x, name, want, dt, dev)
+        return torch.empty_like(x)
+    if not _fit(want, dt, dev.index, x, out):
+        _tensor(x, name, want, dt, dev)
+        _tensor(out, name + " out", want, dt, dev)
+    return out
 
 
 def rotary(shape: B.selkv_shape, plan: B.selkv_rotary, positions: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -336,21 +372,15 @@ def rotary(shape: B.selkv_shape, plan: B.selkv_rotary, positions: torch.Tensor, 
         _bad("rotary: positions [B][T]")
     T, dt = positions.shape[1], _TORCH_DTYPE[shape.dtype]
     _tensor(positions, "rotary: positions", (shape.batch, T), torch.int32, dev)
-    outs = list(out) if out is not None else [None, None]
-    if len(outs) != 2:
-        _bad("rotary: out is (q, k)")
-    for i, (name, x, heads) in enumerate((("q", q, shape.num_q_heads), ("k", k, shape.num_kv_heads))):
-        if x is None:
-            if outs[i] is not None:
-                _bad("rotary: an output without its input")
-            continue
-        _tensor(x, "rotary: " + name, (shape.batch, heads, T, shape.head_dim), dt, dev)
-        if outs[i] is None:
-            outs[i] = torch.empty_like(x)
-        else:
-            _tensor(outs[i], "rotary: out", x.shape, dt, dev)
-    B.check(B.selkv_rotary_apply(shape, plan, T, positions, q, k, outs[0], outs[1], transpose, st), "selkv_rotary_apply")
-    return outs[0], outs[1]
+    qo, ko = out if out is not None else (None, None)
+    if q is not None:
+        qo = _rotary_pair("rotary: q", q, qo, (shape.batch, shape.num_q_heads, T, shape.head_dim), dt, dev)
+    if k is not None:
+        ko = _rotary_pair("rotary: k", k, ko, (shape.batch, shape.num_kv_heads, T, shape.head_dim), dt, dev)
+    if (q is None and qo is not None) or (k is None and ko is not None):
+        _bad("rotary: an output without its input")
+    B.check(B.selkv_rotary_apply(shape, plan, T, positions, q, k, qo, ko, transpose, st), "selkv_rotary_apply")
+    return qo, ko
 
 
 def _tree_tensors(what: str, parents, counts, batch: int, T: int, dev) -> None:
@@ -373,23 +403,18 @@ def tree_attn(cache: CompressedCache, q: torch.Tensor, k_new: torch.Tensor, v_ne
     st = _raw_stream(dev.index)
     T, dt = q.shape[2] if q.dim() == 4 else 0, _TORCH_DTYPE[s.dtype]
     want, new = (s.batch, s.num_q_heads, T, s.head_dim), (s.batch, s.num_kv_heads, T, s.head_dim)
-    rows = (s.batch, s.num_kv_heads, s.m_cap)
-    _tensor(q, "tree_attn: q", want, dt, dev)
-    _tensor(k_new, "tree_attn: k_new", new, dt, dev)
-    _tensor(v_new, "tree_attn: v_new", new, dt, dev)
-    _tensor(cache.K_c, "tree_attn: K_c", rows + (s.head_dim,), dt, dev)
-    _tensor(cache.V_c, "tree_attn: V_c", rows + (s.head_dim,), dt, dev)
-    _tensor(cache.lengths, "tree_attn: lengths", (s.batch,), torch.int32, dev)
-    bias = cache.bias if use_bias else None
-    if bias is not None:
-        _tensor(bias, "tree_attn: bias", rows, torch.float32, dev)
+    if not (_fit(want, dt, dev.index, q) and _fit(new, dt, dev.index, k_new, v_new)):
+        _tensor(q, "tree_attn: q", want, dt, dev)
+        _tensor(k_new, "tree_attn: k_new", new, dt, dev)
+        _tensor(v_new, "tree_attn: v_new", new, dt, dev)
+    _, _, K, V, bias, lengths = _look("tree_attn", cache, bytes(s), dt, dev)
     _tree_tensors("tree_attn", parents, counts, s.batch, T, dev)
     if out is None:
         out = torch.empty_like(q) if counts is None else torch.zeros_like(q)
     else:
         _tensor(out, "tree_attn: out", want, dt, dev)
     ws = _space(workspace, lambda sh: B.selkv_tree_attn_workspace_size(sh, T), s, dev, st)
-    B.check(B.selkv_tree_attn(s, T, parents, counts, q, cache.K_c, cache.V_c, bias, cache.lengths, k_new, v_new, out, ws.buf,
+    B.check(B.selkv_tree_attn(s, T, parents, counts, q, K, V, bias if use_bias else None, lengths, k_new, v_new, out, ws.buf,
                               ws.nbytes, st), "selkv_tree_attn")
     return out
 
@@ -407,16 +432,19 @@ def tree_verify(tokens: torch.Tensor, parents: Optional[torch.Tensor], uniforms:
     if target.dim() != 3:
         _bad("tree_verify: target [B][T][V]")
     n, T, V = target.shape
-    _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
-    if draft is not None:
+    if draft is None:
+        _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
+    elif not _fit((n, T, V), torch.float32, dev.index, target, draft):
+        _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
         _tensor(draft, "tree_verify: draft", (n, T, V), torch.float32, dev)
     _tensor(tokens, "tree_verify: tokens", (n, T), torch.int32, dev)
     _tensor(uniforms, "tree_verify: uniforms", (n, T), torch.float32, dev)
     _tree_tensors("tree_verify", parents, counts, n, T, dev)
     if out is None:
         out = tuple(torch.empty(shape, dtype=torch.int32, device=dev) for shape in ((n,), (n, T), (n,)))
-    for t, shape in zip(out, ((n,), (n, T), (n,))):
-        _tensor(t, "tree_verify: out", shape, torch.int32, dev)
+    else:
+        for t, shape in zip(out, ((n,), (n, T), (n,))):
+            _tensor(t, "tree_verify: out", shape, torch.int32, dev)
     ws = _space(workspace, lambda _: B.selkv_tree_verify_workspace_size(n, T, V), None, dev, st)
     accepted, path, next_token = out
     B.check(B.selkv_tree_verify(n, T, parents, counts, V, tokens, uniforms, target, draft, accepted, path, next_token, ws.buf,
@@ -442,18 +470,17 @@ def tree_commit(caches, K_new, V_new, path: torch.Tensor, accepted: torch.Tensor
     T, dt = path.shape[1], _TORCH_DTYPE[s.dtype]
     _tensor(path, "tree_commit: path", (s.batch, T), torch.int32, dev)
     _tensor(accepted, "tree_commit: accepted", (s.batch,), torch.int32, dev)
-    rows, new = (s.batch, s.num_kv_heads, s.m_cap), (s.batch, s.num_kv_heads, T, s.head_dim)
-    for c, k, v in zip(caches, K_new, V_new):
-        if bytes(c.shape) != bytes(s):
+    new, same = (s.batch, s.num_kv_heads, T, s.head_dim), bytes(s)
+    for name, x in (("tree_commit: K_new", K_new), ("tree_commit: V_new", V_new)):
+        if not _fit(new, dt, dev.index, *x):
+            for t in x:
+                _tensor(t, name, new, dt, dev)
+    for c in caches:
+        if c.shape is not s and bytes(c.shape) != same:
             _bad("tree_commit: caches of one shape")
-        _tensor(c.K_c, "tree_commit: K_c", rows + (s.head_dim,), dt, dev)
-        _tensor(c.V_c, "tree_commit: V_c", rows + (s.head_dim,), dt, dev)
-        _tensor(c.lengths, "tree_commit: lengths", (s.batch,), torch.int32, dev)
-        if c.bias is not None:
-            _tensor(c.bias, "tree_commit: bias", rows, torch.float32, dev)
-        _tensor(k, "tree_commit: K_new", new, dt, dev)
-        _tensor(v, "tree_commit: V_new", new, dt, dev)
+    held = [_look("tree_commit", c, same, dt, dev) for c in caches]
     ws = _space(workspace, B.selkv_tree_commit_workspace_size, s, dev, st)
-    B.check(B.selkv_tree_commit(s, T, path, accepted, K_new, V_new, [c.K_c for c in caches], [c.V_c for c in caches],
-                                [c.bias for c in caches], [c.lengths for c in caches], ws.buf, ws.nbytes, st),
-            "selkv_tree_commit")
+    table = B.c_vp * len(held)
+    K, V, bias, lengths = (table(*x) for x in list(zip(*held))[2:])
+    rows = [table(*[t.data_ptr() for t in x]) for x in (K_new, V_new)]
+    B.check(B.selkv_tree_commit(s, T, path, accepted, *rows, K, V, bias, lengths, ws.buf, ws.nbytes, st), "selkv_tree_commit")

@@ -4,16 +4,15 @@
 // turn per position, and the product's wrap modulo 2^64 takes whole turns off exactly: its upper half is the angle in
 // [-1/2, 1/2) turns, right to 2^-33, for any 32-bit position, without 64-bit floating point (which this GPU has little of).
 //
-// Bound by memory: each element is read and written once.  A CTA takes a tile of tokens and some of the heads: the
-// sines and cosines of the tile are computed once and shared by its heads.
+// Bound by memory: each element is read and written once.  A thread has the same pairs of one token in all heads of its
+// CTA: their sines and cosines are computed once and stay in its registers.
 #include "tree.cuh"
 
 namespace selkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 16;  // tokens of a tile
-constexpr int kHeads = 8;    // heads that share a tile's angles
+constexpr int kMostHeads = 32, kFewestHeads = 4;  // heads of a CTA
 
 // VEC elements of a thread at a time (16 bytes where the pairs allow it).
 template <typename T, int VEC>
@@ -39,63 +38,54 @@ struct Chunk {
 };
 
 // HALF layout: an item is VEC elements of the first half and their partners; INTERLEAVED: 2 VEC
-// elements in a row, VEC pairs.  Behind the pairs, items of 2 VEC elements that stay.
+// elements in a row, VEC pairs.  Behind the pairs, items of 2 VEC elements that stay.  A thread an item of a token.
 template <typename T, int VEC, bool HALF>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(const __grid_constant__ RotaryArgs a) {
-  __shared__ float2 cs[kTokens][SELKV_ROTARY_MAX_DIM / 2 + 1];
-  const int t0 = blockIdx.x * kTokens, nt = min(kTokens, a.T - t0), b = blockIdx.z;
-  const int half = a.rot / 2;
-  for (int i = threadIdx.x; i < nt * half; i += kThreads) {
-    const int t = i / half, f = i - t * half;
-    const int64_t p = a.positions[(size_t)b * a.T + t0 + t];
-    const int32_t turn = (int32_t)(((uint64_t)p * a.turns[f]) >> 32);
-    float s, c;
-    sincospif((float)turn * 0x1p-31f, &s, &c);
-    cs[t][f] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const __grid_constant__ RotaryArgs a, int nheads) {
+  const int half = a.rot / 2, pairs = half / VEC, items = pairs + (a.D - a.rot) / (2 * VEC), tokens = kThreads / items;
+  const int ti = threadIdx.x / items, it = threadIdx.x - ti * items, t = blockIdx.x * tokens + ti, b = blockIdx.z;
+  if (ti >= tokens || t >= a.T) return;
+  const bool turns = it < pairs;
+  float c[VEC], s[VEC];
+  if (turns) {
+    const int64_t p = a.positions[(size_t)b * a.T + t];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int32_t turn = (int32_t)(((uint64_t)p * a.turns[it * VEC + e]) >> 32);
+      sincospif((float)turn * 0x1p-31f, &s[e], &c[e]);
+      c[e] *= a.amplitude;
+      s[e] *= a.amplitude * a.sign;
+    }
   }
-  __syncthreads();
+  const int e0 = turns && HALF ? it * VEC : turns ? it * 2 * VEC : a.rot + (it - pairs) * 2 * VEC;
+  const int e1 = turns && HALF ? e0 + half : e0 + VEC;
   const int nq = a.q != nullptr ? a.Hq : 0, heads = nq + (a.k != nullptr ? a.Hkv : 0);
-  const int h0 = blockIdx.y * kHeads, nh = min(kHeads, heads - h0);
-  const int pairs = half / VEC, items = pairs + (a.D - a.rot) / (2 * VEC);
-  const int all = nh * nt * items;
-#pragma unroll 2
-  for (int i = threadIdx.x; i < all; i += kThreads) {
-    const int rest = i / items, it = i - rest * items;
-    const int hh = rest / nt, t = rest - hh * nt, h = h0 + hh;
+  const int h0 = blockIdx.y * nheads, h1 = min(heads, h0 + nheads);
+#pragma unroll 4
+  for (int h = h0; h < h1; ++h) {
     const bool isq = h < nq;
-    const size_t row = isq ? ((size_t)b * a.Hq + h) * a.T : ((size_t)b * a.Hkv + (h - nq)) * a.T;
-    const size_t at = (row + t0 + t) * a.D;
+    const size_t at = ((isq ? (size_t)b * a.Hq + h : (size_t)b * a.Hkv + (h - nq)) * a.T + t) * a.D;
     const T* src = static_cast<const T*>(isq ? a.q : a.k) + at;
     T* dst = static_cast<T*>(isq ? a.q_out : a.k_out) + at;
-    const bool turns = it < pairs;
-    const int e0 = turns && HALF ? it * VEC : turns ? it * 2 * VEC : a.rot + (it - pairs) * 2 * VEC;
-    const int e1 = turns && HALF ? e0 + half : e0 + VEC;
     Chunk<T, VEC> x, y;
     x.load(src + e0);
     y.load(src + e1);
     if (turns) {
-      const float2* w = cs[t] + it * VEC;
-      if constexpr (HALF) {
+      if constexpr (HALF || VEC == 1) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const float u = x.x[e], v = y.x[e];
-          const float2 c = w[e];
-          x.x[e] = u * c.x - v * c.y;
-          y.x[e] = v * c.x + u * c.y;
+          x.x[e] = u * c[e] - v * s[e];
+          y.x[e] = v * c[e] + u * s[e];
         }
-      } else if constexpr (VEC == 1) {
-        const float u = x.x[0], v = y.x[0];
-        x.x[0] = u * w[0].x - v * w[0].y;
-        y.x[0] = v * w[0].x + u * w[0].y;
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
-          const float2 c0 = w[e / 2], c1 = w[(VEC + e) / 2];
+          const int f0 = e / 2, f1 = (VEC + e) / 2;
           const float u0 = x.x[e], v0 = x.x[e + 1], u1 = y.x[e], v1 = y.x[e + 1];
-          x.x[e] = u0 * c0.x - v0 * c0.y;
-          x.x[e + 1] = v0 * c0.x + u0 * c0.y;
-          y.x[e] = u1 * c1.x - v1 * c1.y;
-          y.x[e + 1] = v1 * c1.x + u1 * c1.y;
+          x.x[e] = u0 * c[f0] - v0 * s[f0];
+          x.x[e + 1] = v0 * c[f0] + u0 * s[f0];
+          y.x[e] = u1 * c[f1] - v1 * s[f1];
+          y.x[e + 1] = v1 * c[f1] + u1 * s[f1];
         }
       }
     }
@@ -107,9 +97,14 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const __grid_constant_
 template <typename T, int VEC>
 cudaError_t launch(const RotaryArgs& a, cudaStream_t s) {
   const int heads = (a.q != nullptr ? a.Hq : 0) + (a.k != nullptr ? a.Hkv : 0);
-  const dim3 grid((unsigned)((a.T + kTokens - 1) / kTokens), (unsigned)((heads + kHeads - 1) / kHeads), (unsigned)a.B);
-  if (a.layout == SELKV_ROPE_HALF) rotary_kernel<T, VEC, true><<<grid, kThreads, 0, s>>>(a);
-  else rotary_kernel<T, VEC, false><<<grid, kThreads, 0, s>>>(a);
+  const int items = a.rot / (2 * VEC) + (a.D - a.rot) / (2 * VEC), tokens = kThreads / items;
+  const int64_t tiles = (int64_t)((a.T + tokens - 1) / tokens) * a.B;
+  // many heads share a thread's angles, but not so many that SMs stay empty
+  int each = kMostHeads;
+  while (each > kFewestHeads && tiles * ((heads + each - 1) / each) < 4 * kPlanSMs) each /= 2;
+  const dim3 grid((unsigned)((a.T + tokens - 1) / tokens), (unsigned)((heads + each - 1) / each), (unsigned)a.B);
+  if (a.layout == SELKV_ROPE_HALF) rotary_kernel<T, VEC, true><<<grid, kThreads, 0, s>>>(a, each);
+  else rotary_kernel<T, VEC, false><<<grid, kThreads, 0, s>>>(a, each);
   return cudaGetLastError();
 }
 
