@@ -44,17 +44,28 @@ constexpr int kTreePieceTiles = 6;
 //   A piece a CTA: a unit of t tiles is cut into ceil(t / share) even pieces, with the smallest share that leaves no more
 //   pieces than CTAs.  Taken where there are no more units than CTAs and that share is at most kTreePieceTiles more, what a
 //   second piece costs (one sequence of 25000 rows, 8 KV heads, 152 CTAs: a CTA with two pieces took 36 us, the others 25).
-// In shared memory: the sequences' (cached rows, tokens), and the pieces or tiles of the sequences before each.
+// In shared memory: the CTA's first piece, the sequences' (cached rows, tokens), and the pieces or tiles of the sequences
+// before each.
+struct TreePiece {
+  int b, kv, blk;
+  int L, n;          // cached rows, tokens
+  int tiles;         // key tiles of the unit
+  int first, count;  // tiles first .. first + count - 1 of it
+  int left;          // places of the CTA's part of the list from here on, this piece's among them
+  __device__ __forceinline__ bool whole() const { return count == tiles; }
+};
 struct TreeList {
-  int32_t* before;  // [B + 1]
+  TreePiece* first;
   int2* seq;        // [B]
+  int32_t* before;  // [B + 1]
   int32_t* head;    // [2] share, 1: a piece a CTA
 };
-__host__ __device__ constexpr int tree_list_bytes(int B) { return (B + 1) * 12 + 12; }  // (before lies behind seq)
+__host__ __device__ constexpr int tree_list_bytes(int B) { return 40 + B * 12 + 12; }
 __device__ __forceinline__ TreeList tree_list_at(void* smem, int B) {  // 8-byte aligned
-  int2* seq = static_cast<int2*>(smem);
+  static_assert(sizeof(TreePiece) <= 40, "the piece comes first");
+  int2* seq = reinterpret_cast<int2*>(static_cast<char*>(smem) + 40);
   int32_t* before = reinterpret_cast<int32_t*>(seq + B);
-  return {before, seq, before + B + 1};
+  return {static_cast<TreePiece*>(smem), seq, before, before + B + 1};
 }
 template <int KEYS>
 __device__ __forceinline__ int tree_tiles(int2 seq) {
@@ -76,14 +87,14 @@ __device__ __forceinline__ void tree_prefix(int32_t* before, int B) {
     sum += __shfl_sync(0xffffffffu, x, 31);
   }
 }
-// All threads of the CTA come here; `tell`: this CTA reports lengths and counts out of range.
+// All threads of the CTA come here.  (The first CTA reports lengths and counts out of range.)
 template <int KEYS>
-__device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, int ctas, bool tell) {
+__device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, int cta, int ctas) {
   const int per = a.Hkv * a.blocks;  // units of a sequence
   for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
     int L = a.lengths[b], n = a.counts != nullptr ? a.counts[b] : a.T;
     if (L < 0 || L > a.m_cap || n < 0 || n > a.T) {
-      if (tell) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
+      if (cta == 0) raise_flag(a.flags, SELKV_DEVERR_LENGTH);
       L = min(max(L, 0), a.m_cap);
       n = min(max(n, 0), a.T);
     }
@@ -125,67 +136,65 @@ __device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, 
     }
     __syncwarp();
     tree_prefix(w.before, a.B);
+    __syncwarp();
+    // the CTA's part of the list, and its first piece
+    const int places = w.before[a.B];
+    const int pos = piece ? min(cta, places) : (int)min((long long)places, (long long)cta * share);
+    const int end = piece ? min(cta + 1, places) : min(places, pos + share);
+    int b = 0;  // before[b] <= pos < before[b + 1]
+    for (int b0 = 0; b0 < a.B; b0 += 32) b += __popc(__ballot_sync(0xffffffffu, b0 + lane < a.B && w.before[b0 + lane + 1] <= pos));
+    if (lane == 0) {
+      TreePiece p{};
+      p.left = end - pos;
+      if (p.left > 0) {
+        const int2 q = w.seq[b];
+        p.b = b;
+        p.L = q.x;
+        p.n = q.y;
+        p.tiles = tree_tiles<KEYS>(q);
+        const int at = pos - w.before[b], pieces = piece ? (p.tiles + share - 1) / share : p.tiles, unit = at / pieces;
+        const int j = at - unit * pieces;
+        if (piece) {
+          const int each = p.tiles / pieces, more = p.tiles - each * pieces;  // `more` pieces have one more
+          p.first = j * each + min(j, more);
+          p.count = each + (j < more ? 1 : 0);
+        } else {
+          p.first = j;
+          p.count = min(p.tiles - j, p.left);
+        }
+        p.kv = unit / a.blocks;
+        p.blk = unit - p.kv * a.blocks;
+      }
+      *w.first = p;
+    }
   }
   __syncthreads();
+}
+// The piece behind `p`: the next unit's first tiles (a CTA with a single place has no other piece).
+template <int KEYS>
+__device__ __forceinline__ void tree_next(const TreeArgs& a, const TreeList& w, TreePiece& p) {
+  p.left -= w.head[1] ? 1 : p.count;
+  if (p.left <= 0) return;
+  if (++p.blk == a.blocks) {
+    p.blk = 0;
+    if (++p.kv == a.Hkv) {
+      p.kv = 0;
+      do ++p.b;
+      while (w.before[p.b + 1] == w.before[p.b]);  // (the list goes on)
+      const int2 s = w.seq[p.b];
+      p.L = s.x;
+      p.n = s.y;
+      p.tiles = tree_tiles<KEYS>(s);
+    }
+  }
+  p.first = 0;
+  p.count = min(p.tiles, p.left);
 }
 // The list for the kernel that joins (by one CTA).
 __device__ __forceinline__ void tree_list_store(const TreeArgs& a, const TreeList& w) {
   for (int b = threadIdx.x; b < a.B + 3; b += blockDim.x) a.before[b] = w.before[b];  // (head lies behind)
 }
 
-// The CTA's part: places pos .. end - 1 of the list.
-struct TreeRange {
-  int pos, end;
-};
-__device__ __forceinline__ TreeRange tree_range(const TreeArgs& a, const TreeList& w, int cta) {
-  const int total = w.before[a.B];
-  if (w.head[1]) return {min(cta, total), min(cta + 1, total)};
-  const int p = (int)min((long long)total, (long long)cta * w.head[0]);
-  return {p, min(total, p + w.head[0])};
-}
-// One piece: tiles first .. first + count - 1 of a unit.
-struct TreePiece {
-  int b, kv, blk;
-  int L, n;      // cached rows, tokens
-  int tiles;     // key tiles of the unit
-  int first, count;
-  int places;    // of the list
-  __device__ __forceinline__ bool whole() const { return count == tiles; }
-};
-// (Not inlined: every role of a CTA asks, and a launch begins with fetching its code, at about a byte a cycle.)
-template <int KEYS>
-__device__ __noinline__ TreePiece tree_piece(const TreeArgs& a, const TreeList& w, TreeRange r) {
-  int lo = 0, hi = a.B;  // before[lo] <= pos < before[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (w.before[mid] <= r.pos) lo = mid;
-    else hi = mid;
-  }
-  const int2 s = w.seq[lo];
-  TreePiece p;
-  p.tiles = tree_tiles<KEYS>(s);
-  const int at = r.pos - w.before[lo];
-  int unit;
-  if (w.head[1]) {
-    const int pieces = (p.tiles + w.head[0] - 1) / w.head[0];
-    unit = at / pieces;
-    const int j = at - unit * pieces, each = p.tiles / pieces, more = p.tiles - each * pieces;  // `more` pieces have one more
-    p.first = j * each + min(j, more);
-    p.count = each + (j < more ? 1 : 0);
-    p.places = 1;
-  } else {
-    unit = at / p.tiles;
-    p.first = at - unit * p.tiles;
-    p.count = min(p.tiles - p.first, r.end - r.pos);
-    p.places = p.count;
-  }
-  p.b = lo;
-  p.kv = unit / a.blocks;
-  p.blk = unit - p.kv * a.blocks;
-  p.L = s.x;
-  p.n = s.y;
-  return p;
-}
 __device__ __forceinline__ float* tree_record(const TreeArgs& a, int cta, const TreePiece& p) {
   return a.partial + (size_t)(cta * 2 + (p.first > 0 ? 0 : 1)) * tree_record_floats(a.rec_rows, a.D);
 }

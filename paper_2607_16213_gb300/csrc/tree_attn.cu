@@ -45,12 +45,9 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
 
   chain_begin();
-  tree_list<KEYS>(a, list, gridDim.x, blockIdx.x == 0);
+  tree_list<KEYS>(a, list, blockIdx.x, gridDim.x);
   if (blockIdx.x == 0) tree_list_store(a, list);
-  TreeRange range = tree_range(a, list, blockIdx.x);
-  while (range.pos < range.end) {
-    const TreePiece p = tree_piece<KEYS>(a, list, range);
-    range.pos += p.places;
+  for (TreePiece p = *list.first; p.left > 0; tree_next<KEYS>(a, list, p)) {
     const size_t bk = (size_t)p.b * a.Hkv + p.kv;
     const int cache_tiles = (p.L + KEYS - 1) / KEYS;
     const int row0 = p.blk * RT, rows = min(RT, a.R - row0);

@@ -197,13 +197,12 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   __syncwarp();
   if (warp == kMmaWarp) tmem_alloc(tmem_slot, kTmemCols);
   pdl_wait();  // (no early start for what follows: its CTAs, waiting, cost this kernel 4 us of 34)
-  tree_list<kKeys>(a, list, gridDim.x, blockIdx.x == 0);
+  tree_list<kKeys>(a, list, blockIdx.x, gridDim.x);
   if (blockIdx.x == 0) tree_list_store(a, list);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const TreeRange range = tree_range(a, list, blockIdx.x);
 
   if (warp == kProducerWarp) {
     if (lane == 0) {
@@ -222,9 +221,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         ++asked;
         return true;
       };
-      for (TreeRange at = range; ok && at.pos < at.end; ++pieces) {
-        const TreePiece p = tree_piece<kKeys>(a, list, at);
-        at.pos += p.places;
+      for (TreePiece p = *list.first; ok && p.left > 0; ++pieces, tree_next<kKeys>(a, list, p)) {
         const int n = p.count, bk = p.b * a.Hkv + p.kv, cache_tiles = (p.L + kKeys - 1) / kKeys;
         // K (or V) of the piece's tile i
         auto load = [&](bool v, int i) -> bool {
@@ -256,7 +253,11 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
           ok = load(true, i);
           if (ok && i + kFirst < n) ok = load(false, i + kFirst);
         }
-        if (C::kQs == 2 && ok && at.pos < at.end) ok = load_q(tree_piece<kKeys>(a, list, at));
+        if (C::kQs == 2 && ok) {
+          TreePiece behind = p;
+          tree_next<kKeys>(a, list, behind);
+          if (behind.left > 0) ok = load_q(behind);
+        }
       }
       if (!ok) {
         *abort_flag = 1;
@@ -269,7 +270,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
     }
   } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
     // ---------------- matrix products of chain c ----------------
-    if (range.pos < range.end) {
+    if (list.first->left > 0) {
       const int c = warp - kMmaWarp;
       bool ok = true;
       const uint32_t leader = elect_one();
@@ -281,9 +282,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         ok = __all_sync(0xffffffffu, !*abort_flag && mbar_wait(bar, parity) && !*abort_flag);
         return ok;
       };
-      for (TreeRange at = range; ok && at.pos < at.end; ++pieces) {
-        const TreePiece p = tree_piece<kKeys>(a, list, at);
-        at.pos += p.places;
+      for (TreePiece p = *list.first; ok && p.left > 0; ++pieces, tree_next<kKeys>(a, list, p)) {
         const int n = p.count, cache_tiles = (p.L + kKeys - 1) / kKeys;
         const bool on = MT == 1 || c == 0 || a.R - p.blk * 256 > 128;  // (rows for the second accumulator)
         auto cols = [&](int i) {
@@ -350,9 +349,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
   } else if (warp == kTreeWarp) {
     // ---------------- the ancestors, a piece ahead of the softmax ----------------
     int trees = 0;
-    for (TreeRange at = range; at.pos < at.end;) {
-      const TreePiece p = tree_piece<kKeys>(a, list, at);
-      at.pos += p.places;
+    for (TreePiece p = *list.first; p.left > 0; tree_next<kKeys>(a, list, p)) {
       if (p.first + p.count <= (p.L + kKeys - 1) / kKeys) continue;
       const int k = trees & 1;
       if (trees >= 2 && (!__all_sync(0xffffffffu, mbar_wait(&tfree[k], ((trees >> 1) & 1) ^ 1) && !*abort_flag))) {
@@ -401,15 +398,18 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
       for (int k = 0; k < 2; ++k) bnext[k] = i < p.count && key0 + k * 32 < p.L ? bias[key0 + k * 32] : -INFINITY;
     };
     const int i0 = MT == 1 ? c : 0, step = MT == 1 ? 2 : 1;
-    TreeRange at = range;
-    if (at.pos < at.end) fetch_bias(tree_piece<kKeys>(a, list, at), i0);
-    while (at.pos < at.end) {
-      const TreePiece p = tree_piece<kKeys>(a, list, at);
-      at.pos += p.places;
+    if (list.first->left > 0) fetch_bias(*list.first, i0);
+    for (TreePiece p = *list.first; p.left > 0; tree_next<kKeys>(a, list, p)) {
       // bias of the chain's tile behind tile i, be it the next piece's
       auto fetch_behind = [&](int i) {
-        if (i + step < p.count || at.pos >= at.end) fetch_bias(p, i + step);
-        else fetch_bias(tree_piece<kKeys>(a, list, at), i0);
+        if (!added) return;
+        if (i + step < p.count) {
+          fetch_bias(p, i + step);
+        } else {
+          TreePiece behind = p;
+          tree_next<kKeys>(a, list, behind);
+          if (behind.left > 0) fetch_bias(behind, i0);
+        }
       };
       const int n = p.count, cache_tiles = (p.L + kKeys - 1) / kKeys;
       const int row0 = p.blk * 128 * MT, rows = min(128 * MT, a.R - row0);
