@@ -440,11 +440,11 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         if (drafts) warp_wait(&tfull[trees & 1], (trees >> 1) & 1);
         bool ok = warp_wait(&sfull[c * 2 + (j & 1)], (j >> 1) & 1);
         tc_fence_after();
-        if (!plain) {
+        auto void_rows = [&]() {
           // rows of V that have no weight become zeros, and so do elements of drafted tokens' rows that are no
           // numbers (0 times an infinity is none): the epilogue gives those to the tokens that see them.  (Where both
           // chains take the tile, both do so, with the same values.)  Behind the wait for S: the copy that had V's place
-          // before is done.
+          // before is done.  Behind P, too: V comes later than K.
           const int u = base + v_place(MT == 1 ? i >> 1 : i, chain_tiles<MT>(n, c)), slot = (C::kRings == 2 ? c : 0) * kRing + u % kRing;
           ok = warp_wait(&full[slot], (u / kRing) & 1) && ok;
           const int key = w4 * 16 + (lane & 15);  // a row and, with two halves of d, one of them
@@ -480,7 +480,8 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
           }
           fence_proxy_async_smem();
           __syncwarp();
-        }
+        };
+        if (MT == 2 && !plain) void_rows();
         if (ok && warp_on) {
           // the reference moves to `mx` where that passes it by more than the slack; returns what is added to the logits
           auto settle = [&](float mx) {
@@ -557,38 +558,33 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             // A tile with keys that are out, or of tokens: S is read twice, 16 columns at a time, in a loop that stays
             // one (little code: it runs once or twice a unit).  P's columns lie before the ones read after it.
             const uint32_t* sees = reinterpret_cast<const uint32_t*>(seen + tok) + (key0 >> 5);
+            const bool biased = added && !drafts;
+            // keys that are not out, as bits (a bias behind the last one is -inf)
+            const uint32_t live0 = __ballot_sync(0xffffffffu, lane < keys && !(biased && bw[lane] == -INFINITY));
+            const uint32_t live1 = __ballot_sync(0xffffffffu, 32 + lane < keys && !(biased && bw[32 + lane] == -INFINITY));
             float mx = -INFINITY, neg = 0.f;
 #pragma unroll 1
             for (int k = 0; k < 4 * chunks; ++k) {
               const int q = k < 2 * chunks ? k : k - 2 * chunks;
               float x[16];
               tmem_ld16_issue(ts + q * 16, x);
+              const uint32_t m = (drafts ? sees[q >> 1] : q >= 2 ? live1 : live0) >> ((q & 1) * 16);
               tmem_wait_ld16(x);
-              if (drafts) {
-                const uint32_t m = sees[q >> 1] >> ((q & 1) * 16);
+              if (biased) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = (m & (1u << e)) != 0u ? x[e] * sc : -INFINITY;
+                for (int e = 0; e < 16; e += 4) {
+                  const float4 b4 = lds_f4(smem_u32(bw + q * 16 + e));
+                  x[e] = fmaf(x[e], sc, b4.x);
+                  x[e + 1] = fmaf(x[e + 1], sc, b4.y);
+                  x[e + 2] = fmaf(x[e + 2], sc, b4.z);
+                  x[e + 3] = fmaf(x[e + 3], sc, b4.w);
+                }
               } else {
-                float b[16];
-                if (added) {
 #pragma unroll
-                  for (int e = 0; e < 16; e += 4) {
-                    const float4 b4 = lds_f4(smem_u32(bw + q * 16 + e));
-                    b[e] = b4.x;
-                    b[e + 1] = b4.y;
-                    b[e + 2] = b4.z;
-                    b[e + 3] = b4.w;
-                  }
-                } else {
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) b[e] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const float y = fmaf(x[e], sc, b[e]);
-                  x[e] = b[e] == -INFINITY || q * 16 + e >= keys ? -INFINITY : y;  // (whatever the row holds)
-                }
+                for (int e = 0; e < 16; ++e) x[e] *= sc;
               }
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x[e] = (m & (1u << e)) != 0u ? x[e] : -INFINITY;  // (whatever the row holds)
               if (k < 2 * chunks) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[e]);
@@ -607,6 +603,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
           }
           tmem_wait_st();
         }
+        if (MT == 1 && !plain) void_rows();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&pfull[c * 2 + (j & 1)]);
