@@ -113,11 +113,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
-               "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Place in the ring (a count over the piece's copies) of K and V of the ring's tile i of n: the first two K, then a V and
@@ -129,7 +124,8 @@ __device__ __forceinline__ int v_place(int i, int n) { return i + min(i + kAhead
 template <int MT>
 __device__ __forceinline__ int chain_tiles(int n, int c) { return MT == 1 ? (n + 1 - c) >> 1 : n; }
 
-__device__ __forceinline__ bool unfit16(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
+// The bf16 of a pair that are no numbers, as ones (an exponent of ones carries into the sign's place).
+__device__ __forceinline__ uint32_t unfit2(uint32_t pair) { return ((((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu; }
 
 template <int D, int MT>
 __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
@@ -432,12 +428,21 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         bool plain = !drafts && keys == kKeys;
         if (added) {
           plain = plain && !__any_sync(0xffffffffu, bnext[0] == -INFINITY || bnext[1] == -INFINITY);
-          bw[lane] = bnext[0];
-          bw[32 + lane] = bnext[1];
+          bw[lane] = drafts ? 0.f : bnext[0];
+          bw[32 + lane] = drafts ? 0.f : bnext[1];
           fetch_behind(i);
           __syncwarp();
         }
-        if (drafts) warp_wait(&tfull[trees & 1], (trees >> 1) & 1);
+        uint32_t live[2];  // where the tile is not plain: the columns that the row sees, as bits
+        if (drafts) {
+          warp_wait(&tfull[trees & 1], (trees >> 1) & 1);
+          const uint2 sees = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint32_t*>(seen + tok) + (key0 >> 5));
+          live[0] = sees.x;
+          live[1] = sees.y;
+        } else if (!plain) {
+          live[0] = __ballot_sync(0xffffffffu, lane < keys && !(added && bw[lane] == -INFINITY));
+          live[1] = __ballot_sync(0xffffffffu, 32 + lane < keys && !(added && bw[32 + lane] == -INFINITY));
+        }
         bool ok = warp_wait(&sfull[c * 2 + (j & 1)], (j >> 1) & 1);
         tc_fence_after();
         auto void_rows = [&]() {
@@ -452,29 +457,22 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             uint4* v = reinterpret_cast<uint4*>(ring + slot * C::kSlot + (lane >> 4) * (kKeys * 128) + key * 128);
             if (key >= keys || (added && !drafts && bw[key] == -INFINITY)) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] = make_uint4(0u, 0u, 0u, 0u);
+              for (int e = 0; e < 8; ++e) v[e ^ (lane & 7)] = make_uint4(0u, 0u, 0u, 0u);  // (the lanes' rows lie 128 bytes apart)
             } else if (drafts) {
-#pragma unroll 1
-              for (int e = 0; e < 8; ++e) {
-                const uint4 x = v[e];
-                uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                bool hit = false;
+              uint32_t hit = 0;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  if (unfit16(w[k])) {
-                    w[k] &= 0xffff0000u;
-                    hit = true;
-                  }
-                  if (unfit16(w[k] >> 16)) {
-                    w[k] &= 0x0000ffffu;
-                    hit = true;
-                  }
+              for (int e = 0; e < 8; ++e) {
+                const uint4 w = v[e ^ (lane & 7)];
+                hit |= unfit2(w.x) | unfit2(w.y) | unfit2(w.z) | unfit2(w.w);
+              }
+              if (hit != 0) {
+                atomicOr(&bad[(key0 + key) >> 5], 1u << (key & 31));
+                __threadfence_block();  // (the other chain may find the element gone)
+#pragma unroll 1
+                for (int e = 0; e < 8; ++e) {
+                  const uint4 w = v[e];
+                  v[e] = make_uint4(w.x & ~unfit2(w.x), w.y & ~unfit2(w.y), w.z & ~unfit2(w.z), w.w & ~unfit2(w.w));
                 }
-                if (hit) {
-                  atomicOr(&bad[(key0 + key) >> 5], 1u << (key & 31));
-                  __threadfence_block();  // (the other chain may find the element gone)
-                }
-                v[e] = make_uint4(w[0], w[1], w[2], w[3]);
               }
             }
           }
@@ -507,100 +505,56 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
             fresh = false;
             return -ref * to2;
           };
-          if (plain) {
-            float x[2][32];
+          float x[2][32];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) tmem_ld32_issue(ts + q * 32, x[q]);
-            float mx = -INFINITY;
+          for (int q = 0; q < 2; ++q) tmem_ld32_issue(ts + q * 32, x[q]);
+          float mx = -INFINITY;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              tmem_wait_ld32(x[q]);
-              if (added) {
-                const uint32_t ba = smem_u32(bw + q * 32);
-                const uint64_t sc2 = pack_f2(sc, sc);
-#pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                  const float4 b4 = lds_f4(ba + e * 4);
-                  unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), sc2, pack_f2(b4.x, b4.y)), x[q][e], x[q][e + 1]);
-                  unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), sc2, pack_f2(b4.z, b4.w)), x[q][e + 2], x[q][e + 3]);
-                }
-              }
-              mx = fmaxf(mx, max32(x[q]));
-            }
-            // (without a bias the scale, which is positive, goes in with the reference)
-            const float neg = settle(added ? mx : mx * sc), by = added ? kLog2e : sc;
-            const uint64_t neg2 = pack_f2(neg, neg), by2 = pack_f2(by, by);
-            uint64_t s01 = pack_f2(0.f, 0.f), s23 = s01;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              uint32_t w[16];
+          for (int q = 0; q < 2; ++q) {
+            tmem_wait_ld32(x[q]);
+            if (added) {
+              const uint32_t ba = smem_u32(bw + q * 32);
+              const uint64_t sc2 = pack_f2(sc, sc);
 #pragma unroll
               for (int e = 0; e < 32; e += 4) {
-                float y0, y1, y2, y3;
-                unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), by2, neg2), y0, y1);
-                unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), by2, neg2), y2, y3);
-                y0 = ex2_approx(y0);
-                y1 = ex2_approx(y1);
-                y2 = ex2_approx(y2);
-                y3 = ex2_approx(y3);
-                s01 = fadd2(s01, pack_f2(y0, y1));
-                s23 = fadd2(s23, pack_f2(y2, y3));
-                w[e / 2] = pack_bf16(y0, y1);
-                w[e / 2 + 1] = pack_bf16(y2, y3);
-              }
-              tmem_st16(ts + q * 16, w);
-            }
-            float a0, a1, a2, a3;
-            unpack_f2(s01, a0, a1);
-            unpack_f2(s23, a2, a3);
-            sum += (a0 + a1) + (a2 + a3);
-          } else {
-            // A tile with keys that are out, or of tokens: S is read twice, 16 columns at a time, in a loop that stays
-            // one (little code: it runs once or twice a unit).  P's columns lie before the ones read after it.
-            const uint32_t* sees = reinterpret_cast<const uint32_t*>(seen + tok) + (key0 >> 5);
-            const bool biased = added && !drafts;
-            // keys that are not out, as bits (a bias behind the last one is -inf)
-            const uint32_t live0 = __ballot_sync(0xffffffffu, lane < keys && !(biased && bw[lane] == -INFINITY));
-            const uint32_t live1 = __ballot_sync(0xffffffffu, 32 + lane < keys && !(biased && bw[32 + lane] == -INFINITY));
-            float mx = -INFINITY, neg = 0.f;
-#pragma unroll 1
-            for (int k = 0; k < 4 * chunks; ++k) {
-              const int q = k < 2 * chunks ? k : k - 2 * chunks;
-              float x[16];
-              tmem_ld16_issue(ts + q * 16, x);
-              const uint32_t m = (drafts ? sees[q >> 1] : q >= 2 ? live1 : live0) >> ((q & 1) * 16);
-              tmem_wait_ld16(x);
-              if (biased) {
-#pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                  const float4 b4 = lds_f4(smem_u32(bw + q * 16 + e));
-                  x[e] = fmaf(x[e], sc, b4.x);
-                  x[e + 1] = fmaf(x[e + 1], sc, b4.y);
-                  x[e + 2] = fmaf(x[e + 2], sc, b4.z);
-                  x[e + 3] = fmaf(x[e + 3], sc, b4.w);
-                }
-              } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] *= sc;
-              }
-#pragma unroll
-              for (int e = 0; e < 16; ++e) x[e] = (m & (1u << e)) != 0u ? x[e] : -INFINITY;  // (whatever the row holds)
-              if (k < 2 * chunks) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, x[e]);
-                if (k == 2 * chunks - 1) neg = settle(mx);
-              } else {
-                uint32_t w[8];
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-                  const float y0 = ex2_approx(fmaf(x[e], to2, neg)), y1 = ex2_approx(fmaf(x[e + 1], to2, neg));
-                  sum += y0 + y1;
-                  w[e / 2] = pack_bf16(y0, y1);
-                }
-                tmem_st8(ts + q * 8, w);
+                const float4 b4 = lds_f4(ba + e * 4);
+                unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), sc2, pack_f2(b4.x, b4.y)), x[q][e], x[q][e + 1]);
+                unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), sc2, pack_f2(b4.z, b4.w)), x[q][e + 2], x[q][e + 3]);
               }
             }
+            if (!plain) {  // (whatever S and the bias are there)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[q][e] = (live[q] & (1u << e)) != 0u ? x[q][e] : -INFINITY;
+            }
+            mx = fmaxf(mx, max32(x[q]));
           }
+          // (without a bias the scale, which is positive, goes in with the reference)
+          const float neg = settle(added ? mx : mx * sc), by = added ? kLog2e : sc;
+          const uint64_t neg2 = pack_f2(neg, neg), by2 = pack_f2(by, by);
+          uint64_t s01 = pack_f2(0.f, 0.f), s23 = s01;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              float y0, y1, y2, y3;
+              unpack_f2(ffma2(pack_f2(x[q][e], x[q][e + 1]), by2, neg2), y0, y1);
+              unpack_f2(ffma2(pack_f2(x[q][e + 2], x[q][e + 3]), by2, neg2), y2, y3);
+              y0 = ex2_approx(y0);
+              y1 = ex2_approx(y1);
+              y2 = ex2_approx(y2);
+              y3 = ex2_approx(y3);
+              s01 = fadd2(s01, pack_f2(y0, y1));
+              s23 = fadd2(s23, pack_f2(y2, y3));
+              w[e / 2] = pack_bf16(y0, y1);
+              w[e / 2 + 1] = pack_bf16(y2, y3);
+            }
+            tmem_st16(ts + q * 16, w);
+          }
+          float a0, a1, a2, a3;
+          unpack_f2(s01, a0, a1);
+          unpack_f2(s23, a2, a3);
+          sum += (a0 + a1) + (a2 + a3);
           tmem_wait_st();
         }
         if (MT == 1 && !plain) void_rows();
