@@ -240,6 +240,45 @@ def test_tree_attn_many_short_sequences(dtype):
     c.check(c.run(out=before.clone()), before=before)
 
 
+@pytest.mark.parametrize("dtype,B,hq,hkv,d,cap,T", [
+    ("bf16", 40, 32, 4, 128, 300, 20), ("bf16", 70, 16, 2, 64, 200, 40), ("bf16", 6, 16, 1, 128, 130, 128),
+    ("bf16", 300, 8, 8, 128, 90, 3), ("bf16", 1024, 2, 1, 64, 40, 2), ("fp32", 1024, 2, 1, 64, 40, 2),
+    ("fp32", 20, 16, 1, 128, 100, 30)])
+def test_tree_attn_several_units_a_cta(dtype, B, hq, hkv, d, cap, T):
+    """More units than CTAs: a CTA ends some and begins others, and what two share is joined."""
+    rng = np.random.default_rng(11)
+    c = Case(dtype, B, hq, hkv, d, cap, [int(x) for x in rng.integers(0, cap + 1, B)], T, [int(x) for x in rng.integers(0, T + 1, B)],
+             bias="masked")
+    before = torch.full_like(c.q, 3.0)
+    ws = api.Workspace(S.selkv_tree_attn_workspace_size(c.shape, T))
+    out = c.run(out=before.clone(), workspace=ws)
+    c.check(out, before=before)
+    assert ws.errors() == 0
+    assert torch.equal(c.run(out=before.clone(), workspace=ws), out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_offsets_past_32_bits(dtype):
+    """The last head's rows begin past 2^31 elements.  The work is cut by the lengths alone: to the bit what a small cache
+    gives."""
+    H, d, L, T, far = 8, 128, 777, 6, 2_500_000
+    small = Case(dtype, 1, 16, H, d, 1000, [L], T, None)
+    want = small.run()
+    shape = api.make_shape(dtype, 1, 16, H, d, 8, far, far)
+    big = api.CompressedCache(shape, *(torch.empty((1, H, far, d), dtype=DT[dtype], device="cuda") for _ in range(2)),
+                              torch.empty((1, H, far), device="cuda"), small.cache.lengths.clone())
+    for to, x in ((big.K_c, small.cache.K_c), (big.V_c, small.cache.V_c), (big.bias, small.cache.bias)):
+        to[:, :, :L] = x[:, :, :L]
+        to[:, :, L:L + 200] = math.nan
+    assert torch.equal(api.tree_attn(big, small.q, small.k, small.v, small.parents), want)
+    path, accepted = dev(np.array([[0, 2, 3, 5, -1, -1]]), torch.int32), dev(np.array([4]), torch.int32)
+    api.tree_commit(big, small.k, small.v, path, accepted)
+    at = [0, 2, 3, 5]
+    assert int(big.lengths[0]) == L + 4
+    assert torch.equal(big.K_c[0, :, L:L + 4], small.k[0][:, at]) and torch.equal(big.V_c[0, :, L:L + 4], small.v[0][:, at])
+    assert (big.bias[0, :, L:L + 4] == 0).all() and big.bias[0, :, L + 4:L + 200].isnan().all() and big.K_c[0, :, L + 4:L + 200].isnan().all()
+
+
 @pytest.mark.parametrize("dtype,T,hq", [("bf16", 4, 8), ("bf16", 24, 8), ("bf16", 64, 8), ("fp32", 3, 4), ("fp32", 24, 4)])
 def test_tree_attn_long_cache(dtype, T, hq):
     c = Case(dtype, 1, hq, 2, 128, 20000, [19937], T, None)
@@ -423,6 +462,11 @@ def test_tree_verify(drawn, B, T, V):
         got = run_verify(tokens, parents, u, target, draft if drawn else None, counts, ws)
         check_verify(got, tokens, parents, u, target, draft if drawn else None, counts)
         assert ws.errors() == 0
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_tree_verify_largest_vocabulary(drawn):
+    test_tree_verify(drawn, 1, 4, 1 << 20)
 
 
 @pytest.mark.parametrize("V", [8, 4096, 40000])
