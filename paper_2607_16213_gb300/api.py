@@ -317,7 +317,7 @@ def rotary_plan(rot_dim: int, theta: float = 10000.0, layout: str = "half", scal
     return plan
 
 
-def _fit(shape, dtype, index: int, *tensors) -> bool:
+def _fit(shape, dtype, index: int, tensors) -> bool:
     """Whether all of `tensors` are contiguous, of that shape and type, on that device (`_tensor` says which is not)."""
     for t in tensors:
         if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
@@ -325,22 +325,19 @@ def _fit(shape, dtype, index: int, *tensors) -> bool:
     return True
 
 
-def _look(what: str, c: CompressedCache, key: bytes, dt, dev) -> tuple:
-    """The addresses of the tensors of a cache with the shape whose bytes are `key`; they are looked over when they are
-    others than the last time: other tensors, other memory or another shape."""
-    s = c.shape
-    K, V, b, n = c.K_c, c.V_c, c.bias, c.lengths
-    now = (key, dev, K.data_ptr(), V.data_ptr(), b.data_ptr() if b is not None else None, n.data_ptr())
-    seen = c.__dict__.get("_seen")
-    if seen is None or seen[0] != now or seen[1] is not K or seen[2] is not V or seen[3] is not b or seen[4] is not n:
-        rows = (s.batch, s.num_kv_heads, s.m_cap)
-        _tensor(K, what + ": K_c", rows + (s.head_dim,), dt, dev)
-        _tensor(V, what + ": V_c", rows + (s.head_dim,), dt, dev)
-        _tensor(n, what + ": lengths", (s.batch,), torch.int32, dev)
-        if b is not None:
-            _tensor(b, what + ": bias", rows, torch.float32, dev)
-        c._seen = (now, K, V, b, n)
-    return now
+def _held(what: str, caches, dt, dev) -> tuple:
+    """The tensors of caches of the first one's shape, looked over: their K_c, V_c, bias and lengths."""
+    s = caches[0].shape
+    rows = (s.batch, s.num_kv_heads, s.m_cap)
+    K, V, bias, lengths = [c.K_c for c in caches], [c.V_c for c in caches], [c.bias for c in caches], [c.lengths for c in caches]
+    given = [b for b in bias if b is not None]
+    if not (_fit(rows + (s.head_dim,), dt, dev.index, K + V) and _fit((s.batch,), torch.int32, dev.index, lengths)
+            and _fit(rows, torch.float32, dev.index, given)):
+        for name, x, want, kind in (("K_c", K, rows + (s.head_dim,), dt), ("V_c", V, rows + (s.head_dim,), dt),
+                                    ("lengths", lengths, (s.batch,), torch.int32), ("bias", given, rows, torch.float32)):
+            for t in x:
+                _tensor(t, "%s: %s" % (what, name), want, kind, dev)
+    return K, V, bias, lengths
 
 
 def _cuda(t: torch.Tensor, name: str) -> torch.device:
@@ -353,7 +350,7 @@ def _rotary_pair(name: str, x: torch.Tensor, out: Optional[torch.Tensor], want, 
     if out is None:
         _tensor(x, name, want, dt, dev)
         return torch.empty_like(x)
-    if not _fit(want, dt, dev.index, x, out):
+    if not _fit(want, dt, dev.index, (x, out)):
         _tensor(x, name, want, dt, dev)
         _tensor(out, name + " out", want, dt, dev)
     return out
@@ -403,11 +400,11 @@ def tree_attn(cache: CompressedCache, q: torch.Tensor, k_new: torch.Tensor, v_ne
     st = _raw_stream(dev.index)
     T, dt = q.shape[2] if q.dim() == 4 else 0, _TORCH_DTYPE[s.dtype]
     want, new = (s.batch, s.num_q_heads, T, s.head_dim), (s.batch, s.num_kv_heads, T, s.head_dim)
-    if not (_fit(want, dt, dev.index, q) and _fit(new, dt, dev.index, k_new, v_new)):
+    if not (_fit(want, dt, dev.index, (q,)) and _fit(new, dt, dev.index, (k_new, v_new))):
         _tensor(q, "tree_attn: q", want, dt, dev)
         _tensor(k_new, "tree_attn: k_new", new, dt, dev)
         _tensor(v_new, "tree_attn: v_new", new, dt, dev)
-    _, _, K, V, bias, lengths = _look("tree_attn", cache, bytes(s), dt, dev)
+    (K,), (V,), (bias,), (lengths,) = _held("tree_attn", [cache], dt, dev)
     _tree_tensors("tree_attn", parents, counts, s.batch, T, dev)
     if out is None:
         out = torch.empty_like(q) if counts is None else torch.zeros_like(q)
@@ -434,7 +431,7 @@ def tree_verify(tokens: torch.Tensor, parents: Optional[torch.Tensor], uniforms:
     n, T, V = target.shape
     if draft is None:
         _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
-    elif not _fit((n, T, V), torch.float32, dev.index, target, draft):
+    elif not _fit((n, T, V), torch.float32, dev.index, (target, draft)):
         _tensor(target, "tree_verify: target", (n, T, V), torch.float32, dev)
         _tensor(draft, "tree_verify: draft", (n, T, V), torch.float32, dev)
     _tensor(tokens, "tree_verify: tokens", (n, T), torch.int32, dev)
@@ -472,15 +469,17 @@ def tree_commit(caches, K_new, V_new, path: torch.Tensor, accepted: torch.Tensor
     _tensor(accepted, "tree_commit: accepted", (s.batch,), torch.int32, dev)
     new, same = (s.batch, s.num_kv_heads, T, s.head_dim), bytes(s)
     for name, x in (("tree_commit: K_new", K_new), ("tree_commit: V_new", V_new)):
-        if not _fit(new, dt, dev.index, *x):
+        if not _fit(new, dt, dev.index, x):
             for t in x:
                 _tensor(t, name, new, dt, dev)
     for c in caches:
         if c.shape is not s and bytes(c.shape) != same:
             _bad("tree_commit: caches of one shape")
-    held = [_look("tree_commit", c, same, dt, dev) for c in caches]
+    held = _held("tree_commit", caches, dt, dev)
     ws = _space(workspace, B.selkv_tree_commit_workspace_size, s, dev, st)
-    table = B.c_vp * len(held)
-    K, V, bias, lengths = (table(*x) for x in list(zip(*held))[2:])
-    rows = [table(*[t.data_ptr() for t in x]) for x in (K_new, V_new)]
-    B.check(B.selkv_tree_commit(s, T, path, accepted, *rows, K, V, bias, lengths, ws.buf, ws.nbytes, st), "selkv_tree_commit")
+    table = B.c_vp * len(caches)
+    K, V, bias, lengths = held
+    address = torch.Tensor.data_ptr
+    rows = [table(*map(address, x)) for x in (K_new, V_new, K, V)]
+    rows += [table(*[None if b is None else address(b) for b in bias]), table(*map(address, lengths))]
+    B.check(B.selkv_tree_commit(s, T, path, accepted, *rows, ws.buf, ws.nbytes, st), "selkv_tree_commit")
