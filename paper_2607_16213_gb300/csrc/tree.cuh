@@ -32,9 +32,12 @@ struct TreeArgs {
 // sum) [rows].  Rows side by side: the lanes of a warp hold a row each.
 __host__ __device__ constexpr size_t tree_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
-// Fewest tiles of a piece where a unit is cut (below it a partial's way through memory costs more than the tiles).
-constexpr int kTreeMinTiles = 2;
-// What ending one piece and beginning another costs a CTA, in tiles.
+// Fewest tiles of a piece where a unit is cut: below it a partial's way through memory costs more than the tiles do (bf16, 1000 rows
+// x 8 heads, 8 tokens: 1 tile 13.5 us, 2 12.4, 4 12.8; fp32, 2 x 1000 rows x 2 heads, 7 tokens, where a tile takes longer: 1
+// 13.9, 2 17.0, 4 24.3).
+constexpr int kTreeTcMinTiles = 2, kTreeSimtMinTiles = 1;
+// What ending one piece and beginning another costs a CTA, in tiles (bf16, 4 x 5000 rows x 8 heads, 8 tokens: 6 or 12 25.6 us, 0
+// 27.5).
 constexpr int kTreePieceTiles = 6;
 
 // The work is the list of all units (sequence, KV head, row block) and their key tiles: those of the cached rows,
@@ -88,7 +91,7 @@ __device__ __forceinline__ void tree_prefix(int32_t* before, int B) {
   }
 }
 // All threads of the CTA come here.  (The first CTA reports lengths and counts out of range.)
-template <int KEYS>
+template <int KEYS, int MIN>
 __device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, int cta, int ctas) {
   const int per = a.Hkv * a.blocks;  // units of a sequence
   for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
@@ -115,7 +118,7 @@ __device__ __forceinline__ void tree_list(const TreeArgs& a, const TreeList& w, 
       units += __shfl_xor_sync(0xffffffffu, units, o);
       total += __shfl_xor_sync(0xffffffffu, total, o);
     }
-    int share = max(kTreeMinTiles, (total + ctas - 1) / ctas);
+    int share = max(MIN, (total + ctas - 1) / ctas);
     bool piece = false;
     if (units <= ctas) {
       // (a candidate a lane)
@@ -244,12 +247,13 @@ __device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, 
 }
 
 constexpr int kTreeTcKeys = 64, kTreeSimtKeys = 64;  // keys of a tile
-// Rows of a block (tensor cores: two accumulators of 128 rows where one does not hold them).
+// Rows of a block.  Tensor cores: two accumulators of 128 rows where one does not hold them.  CUDA cores: 16 where they hold all (14
+// rows, 2 x 1000 cached ones: blocks of 16 17.0 us, of 64 24.1; 16000: 37.9 and 50.5).
 inline int tree_block_rows(int dtype, int R) {
   if (dtype == SELKV_BF16) return R <= 128 ? 128 : 256;
   return R <= 16 ? 16 : 64;
 }
-int tree_ctas(int dtype, int D, int R);  // CTAs of a launch
+int tree_ctas(int dtype);  // CTAs of a launch
 cudaError_t launch_tree_attn(const TreeArgs& a, cudaStream_t s);
 cudaError_t launch_tree_tc(const TreeArgs& a, int ctas, cudaStream_t s);
 
