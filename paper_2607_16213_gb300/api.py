@@ -341,7 +341,7 @@ def _held(what: str, caches, dt, dev) -> tuple:
 
 
 def _cuda(t: torch.Tensor, name: str) -> torch.device:
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         _bad("%s: a tensor of a CUDA device" % name)
     return t.device
 
@@ -397,19 +397,22 @@ def tree_attn(cache: CompressedCache, q: torch.Tensor, k_new: torch.Tensor, v_ne
     if _elsewhere(dev, stream):
         with _on(dev, stream):
             return tree_attn(cache, q, k_new, v_new, parents, counts, use_bias, out, workspace)
-    st = _raw_stream(dev.index)
-    T, dt = q.shape[2] if q.dim() == 4 else 0, _TORCH_DTYPE[s.dtype]
-    want, new = (s.batch, s.num_q_heads, T, s.head_dim), (s.batch, s.num_kv_heads, T, s.head_dim)
-    if not (_fit(want, dt, dev.index, (q,)) and _fit(new, dt, dev.index, (k_new, v_new))):
-        _tensor(q, "tree_attn: q", want, dt, dev)
-        _tensor(k_new, "tree_attn: k_new", new, dt, dev)
-        _tensor(v_new, "tree_attn: v_new", new, dt, dev)
-    (K,), (V,), (bias,), (lengths,) = _held("tree_attn", [cache], dt, dev)
-    _tree_tensors("tree_attn", parents, counts, s.batch, T, dev)
+    index = dev.index
+    st = _raw_stream(index)
+    T, dt, n, d = q.shape[2] if q.dim() == 4 else 0, _TORCH_DTYPE[s.dtype], s.batch, s.head_dim
+    want, new, rows = (n, s.num_q_heads, T, d), (n, s.num_kv_heads, T, d), (n, s.num_kv_heads, s.m_cap)
+    K, V, bias, lengths = cache.K_c, cache.V_c, cache.bias, cache.lengths
+    if not (_fit(want, dt, index, (q,) if out is None else (q, out)) and _fit(new, dt, index, (k_new, v_new))
+            and _fit(rows + (d,), dt, index, (K, V)) and (bias is None or _fit(rows, torch.float32, index, (bias,)))
+            and _fit((n,), torch.int32, index, (lengths,) if counts is None else (lengths, counts))
+            and (parents is None or _fit((n, T), torch.int32, index, (parents,)))):
+        _held("tree_attn", [cache], dt, dev)
+        for name, t, shape in (("q", q, want), ("k_new", k_new, new), ("v_new", v_new, new), ("out", out, want)):
+            if t is not None:
+                _tensor(t, "tree_attn: " + name, shape, dt, dev)
+        _tree_tensors("tree_attn", parents, counts, n, T, dev)
     if out is None:
         out = torch.empty_like(q) if counts is None else torch.zeros_like(q)
-    else:
-        _tensor(out, "tree_attn: out", want, dt, dev)
     ws = _space(workspace, lambda sh: B.selkv_tree_attn_workspace_size(sh, T), s, dev, st)
     B.check(B.selkv_tree_attn(s, T, parents, counts, q, K, V, bias if use_bias else None, lengths, k_new, v_new, out, ws.buf,
                               ws.nbytes, st), "selkv_tree_attn")
