@@ -13,7 +13,7 @@
 // max(p - A q, 0) with A the sum of the masses that they were taken with (max(max(x, 0) - y, 0) is max(x - y, 0) for
 // y >= 0), so a pass costs the same however many there were.
 //
-// 1 x 32000 entries, 8 tokens: 8 us on the GPU, latencies (tests, pass, draw).  64 x 128000, 16 tokens: 40 us where the rows of the
+// 1 x 32000 entries, 8 tokens: 8 us on the GPU, latencies (tests, pass, draw).  64 x 128000, 16 tokens: 41 us where the rows of the
 // 1.5 passes a sequence takes would need 14: latencies, and sequences with up to four passes (about 25 instructions
 // an entry and pass: 8 us of all issue slots).
 #include "tree.cuh"
@@ -54,6 +54,8 @@ struct Smem {
   u64 qt[SELKV_MAX_TREE];           // draft's
   u64 warp[kWarps];
   u64 part[2];                      // the CTA's sum, read by the cluster
+  float warp_about[kWarps];
+  float about[2];                   // the same in fp32: where it is 4 or more the fixed point has wrapped
   float u[SELKV_MAX_TREE];
   int parent[SELKV_MAX_TREE];
   uint32_t first[SELKV_MAX_TREE / 32];  // tokens that are accepted when no child of their parent was rejected before, as bits
@@ -68,6 +70,11 @@ struct Smem {
 __device__ __forceinline__ u64 ld_peer_u64(uint32_t peer) {
   u64 v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(peer) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_peer_f32(uint32_t peer) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer) : "memory");
   return v;
 }
 __device__ __forceinline__ u64 warp_sum_u64(u64 v) {
@@ -155,7 +162,7 @@ struct Weights {
 // This warp's part of the sum of the weights over the CTA's entries lo .. hi - 1, span by span; two spans' loads are on
 // their way together.
 template <bool DRAWN, int kAfter>
-__device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, bool& bad) {
+__device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, float& about, bool& bad) {
   constexpr int kRows = kSpan / 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, spans = (hi - lo + kSpan - 1) / kSpan;
   u64 mine = 0;
@@ -204,6 +211,7 @@ __device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int 
         w.template onto<kAfter>(sum, a.z, c.z);
         w.template onto<kAfter>(sum, a.w, c.w);
       }
+      about += sum.s;
       const u64 f = warp_sum_u64(sum.fixed());
       if (lane == 0) sm->span[at] = f;
       mine += f;
@@ -217,25 +225,39 @@ template <bool DRAWN>
 __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, int ctas, int& phase, bool& bad) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   u64 mine;
-  if (!DRAWN || w.rejected == 0) mine = sum_spans<DRAWN, 0>(w, sm, lo, hi, bad);
-  else if (w.rejected == 1) mine = sum_spans<DRAWN, 1>(w, sm, lo, hi, bad);
-  else mine = sum_spans<DRAWN, 2>(w, sm, lo, hi, bad);
-  if (lane == 0) sm->warp[warp] = mine;
+  float about = 0.f;
+  if (!DRAWN || w.rejected == 0) mine = sum_spans<DRAWN, 0>(w, sm, lo, hi, about, bad);
+  else if (w.rejected == 1) mine = sum_spans<DRAWN, 1>(w, sm, lo, hi, about, bad);
+  else mine = sum_spans<DRAWN, 2>(w, sm, lo, hi, about, bad);
+  about = warp_sum(about);
+  if (lane == 0) {
+    sm->warp[warp] = mine;
+    sm->warp_about[warp] = about;
+  }
   __syncthreads();
   if (threadIdx.x < 32) {
     const u64 t = warp_sum_u64(threadIdx.x < kWarps ? sm->warp[threadIdx.x] : 0);
-    if (threadIdx.x == 0) sm->part[phase & 1] = t;
+    const float x = warp_sum(threadIdx.x < kWarps ? sm->warp_about[threadIdx.x] : 0.f);
+    if (threadIdx.x == 0) {
+      sm->part[phase & 1] = t;
+      sm->about[phase & 1] = x;
+    }
   }
   cluster_arrive();
   cluster_wait();
   u64 total = 0;
-  for (int c = 0; c < ctas; ++c) total += ld_peer_u64(peer_smem(smem_u32(&sm->part[phase & 1]), c));
+  about = 0.f;
+  for (int c = 0; c < ctas; ++c) {
+    total += ld_peer_u64(peer_smem(smem_u32(&sm->part[phase & 1]), c));
+    about += ld_peer_f32(peer_smem(smem_u32(&sm->about[phase & 1]), c));
+  }
+  bad = bad || about >= 3.99f;
   ++phase;
   return total;
 }
 
 template <bool DRAWN>
-__global__ __launch_bounds__(kThreads) void tree_verify_kernel(VerifyArgs a, int part) {
+__global__ __launch_bounds__(kThreads, 2) void tree_verify_kernel(VerifyArgs a, int part) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   Smem* sm = reinterpret_cast<Smem*>(smem_raw);
   const int tid = threadIdx.x, rank = blockIdx.x, ctas = gridDim.x, b = blockIdx.y;

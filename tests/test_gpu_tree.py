@@ -563,6 +563,19 @@ def test_tree_verify_reports_bad_numbers():
     assert flags == S.SELKV_DEVERR_LENGTH and out[0][0] == 0 and out[2][0] == -1 and (out[1] == -1).all()
 
 
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("V", [5, 700, 40000])
+def test_tree_verify_reports_sums_that_do_not_fit(V, drawn):
+    rng = np.random.default_rng(3)
+    target, draft = (probabilities(rng, (2, 3, V), 1.0) for _ in range(2))
+    target[1] = 1.5  # (sequence 0 stays as it should be)
+    tokens, u = np.array([[0, 1, 2]] * 2), np.full((2, 3), 0.875, dtype=np.float32)
+    ws = api.Workspace(256)
+    out = run_verify(tokens, None, u, target, draft if drawn else None, None, ws)
+    assert ws.errors() == S.SELKV_DEVERR_VALUE and 0 <= out[2][1] < V
+    check_verify([x[:1] for x in out], tokens[:1], None, u[:1], target[:1], draft[:1] if drawn else None)
+
+
 # ---- commit -------------------------------------------------------------------------------------
 def commit_case(dtype, L, B, hkv, d, cap, T, seed=0, bias=True):
     rng = np.random.default_rng(seed)
