@@ -54,8 +54,9 @@ struct Smem {
   u64 qt[SELKV_MAX_TREE];           // draft's
   u64 warp[kWarps];
   u64 part[2];                      // the CTA's sum, read by the cluster
+  float mine[kThreads];             // each thread's sum in fp32 (registers are short)
   float warp_about[kWarps];
-  float about[2];                   // the same in fp32: where it is 4 or more the fixed point has wrapped
+  float about[2];                   // the CTA's in fp32: where the cluster's is 4 or more the fixed point has wrapped
   float u[SELKV_MAX_TREE];
   int parent[SELKV_MAX_TREE];
   uint32_t first[SELKV_MAX_TREE / 32];  // tokens that are accepted when no child of their parent was rejected before, as bits
@@ -162,7 +163,7 @@ struct Weights {
 // This warp's part of the sum of the weights over the CTA's entries lo .. hi - 1, span by span; two spans' loads are on
 // their way together.
 template <bool DRAWN, int kAfter>
-__device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, float& about, bool& bad) {
+__device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, bool& bad) {
   constexpr int kRows = kSpan / 128;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, spans = (hi - lo + kSpan - 1) / kSpan;
   u64 mine = 0;
@@ -211,7 +212,7 @@ __device__ __forceinline__ u64 sum_spans(const Weights<DRAWN>& w, Smem* sm, int 
         w.template onto<kAfter>(sum, a.z, c.z);
         w.template onto<kAfter>(sum, a.w, c.w);
       }
-      about += sum.s;
+      sm->mine[threadIdx.x] += sum.s;
       const u64 f = warp_sum_u64(sum.fixed());
       if (lane == 0) sm->span[at] = f;
       mine += f;
@@ -225,11 +226,11 @@ template <bool DRAWN>
 __device__ u64 sum_weights(const Weights<DRAWN>& w, Smem* sm, int lo, int hi, int ctas, int& phase, bool& bad) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   u64 mine;
-  float about = 0.f;
-  if (!DRAWN || w.rejected == 0) mine = sum_spans<DRAWN, 0>(w, sm, lo, hi, about, bad);
-  else if (w.rejected == 1) mine = sum_spans<DRAWN, 1>(w, sm, lo, hi, about, bad);
-  else mine = sum_spans<DRAWN, 2>(w, sm, lo, hi, about, bad);
-  about = warp_sum(about);
+  sm->mine[threadIdx.x] = 0.f;
+  if (!DRAWN || w.rejected == 0) mine = sum_spans<DRAWN, 0>(w, sm, lo, hi, bad);
+  else if (w.rejected == 1) mine = sum_spans<DRAWN, 1>(w, sm, lo, hi, bad);
+  else mine = sum_spans<DRAWN, 2>(w, sm, lo, hi, bad);
+  float about = warp_sum(sm->mine[threadIdx.x]);
   if (lane == 0) {
     sm->warp[warp] = mine;
     sm->warp_about[warp] = about;
