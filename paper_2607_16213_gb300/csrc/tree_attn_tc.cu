@@ -385,6 +385,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
         *abort_flag = 1;
         raise_flag(a.flags, SELKV_DEVERR_TIMEOUT);
       }
+      __syncwarp();
       return ok;
     };
     int base = 0;        // copies into the chain's ring before the piece
@@ -636,8 +637,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
                 }
               }
           }
-          if (!write) continue;
-          if (whole) {
+          if (write && whole) {
 #pragma unroll
             for (int e = 0; e < 16; e += 8) {
               uint4 w;
@@ -647,14 +647,16 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
               w.w = pack_bf16(o[e + 6] * inv, o[e + 7] * inv);
               *reinterpret_cast<uint4*>(orow + d + e) = w;
             }
-          } else {
+          } else if (write) {
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
               reinterpret_cast<float4*>(rec)[(size_t)((d + e) / 4) * a.rec_rows + r] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
+          __syncwarp();  // (rows that are written and rows that are not go on together: the next loads are the whole warp's)
         }
         if (write && !whole && d0 == 0) reinterpret_cast<float2*>(rec + (size_t)a.rec_rows * D)[r] = make_float2(ref, sum);
         tc_fence_before();
+        __syncwarp();  // (the barrier is, too)
         if (MT == 1) named_bar_sync(pair_bar, 64);  // both chains' O, and the rows' sums, are read
       }
       if (has_drafts) {
@@ -665,6 +667,7 @@ __global__ __launch_bounds__(kThreads, 1) void tree_tc_kernel(const __grid_const
     }
   }
   tc_fence_before();
+  __syncwarp();
   __syncthreads();
   tc_fence_after();
   if (warp == kMmaWarp) tmem_dealloc(tmem, kTmemCols);

@@ -1,0 +1,36 @@
+"""Rules that the kernels of a speculative step keep and no run can show."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_16213_gb300", "csrc")
+
+
+def closing(code, i, pair):
+    """The place behind what closes the bracket before place i."""
+    depth = 1
+    while depth:
+        depth += {pair[0]: 1, pair[1]: -1}.get(code[i], 0)
+        i += 1
+    return i
+
+
+def loops(code):
+    """The bodies of the loops of `code` that have braces."""
+    for m in re.finditer(r"\bfor \(", code):
+        head = closing(code, m.end(), "()")
+        if code[head:].lstrip().startswith("{"):
+            start = code.index("{", head) + 1
+            yield code[start:closing(code, start, "{}") - 1]
+
+
+def test_loads_from_tensor_memory_are_the_whole_warps():
+    """tcgen05.ld and its wait want every lane of the warp at the same instruction.  So no lane leaves an iteration of
+    their loops early, and a loop whose lanes may part gathers them before the next iteration."""
+    code = re.sub(r"//.*", "", open(os.path.join(CSRC, "tree_attn_tc.cu")).read())
+    bodies = [b for b in loops(code) if re.search(r"tmem_ld\d+_issue\(", b) and not any(
+        re.search(r"tmem_ld\d+_issue\(", inner) for inner in loops(b))]
+    assert len(bodies) >= 2
+    for b in bodies:
+        assert "continue;" not in b and "break;" not in b, b
+        if re.search(r"\bif \(", b):
+            assert b.rstrip().endswith("__syncwarp();"), b
