@@ -17,6 +17,7 @@
 // 1.5 passes a sequence takes would need 14: latencies, and sequences with up to four passes (about 25 instructions
 // an entry and pass: 8 us of all issue slots).
 #include "tree.cuh"
+#include "tree_fixed.h"
 
 namespace selkv {
 namespace {
@@ -37,17 +38,6 @@ __device__ __forceinline__ u64 times_fix(u64 A, u64 q) {
   const u64 hi = __umul64hi(A, q), lo = A * q;
   return hi >> kTimes != 0 ? ~0ull : (hi << (64 - kTimes)) | (lo >> kTimes);
 }
-// A probability in fixed point; one that is none counts as 0.
-__device__ __forceinline__ u64 to_fix(float p, bool& bad) {
-  const bool ok = p >= 0.f && p < 2.f;
-  bad = bad || !ok;
-  // the mantissa in its place, by shifts (the conversion instruction runs at a quarter of their rate)
-  const uint32_t u = ok ? __float_as_uint(p) : 0u;
-  const int shift = (int)(u >> 23) - 88;
-  const u64 m = (u & 0x7fffffu) | 0x800000u;
-  return shift >= 0 ? m << shift : shift > -32 ? (u64)((uint32_t)m >> -shift) : 0ull;
-}
-
 struct Smem {
   u64 span[kMaxVocab / kSpan + 1];  // sums of the CTA's spans
   u64 pt[SELKV_MAX_TREE];           // target probability of token t at its parent
