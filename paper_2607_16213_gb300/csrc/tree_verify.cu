@@ -386,6 +386,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_verify_kernel(VerifyArgs a, 
           }
           __syncwarp();
         }
+        __syncwarp();  // (every lane has read the last round's A)
         if (tid == 0) {
           sm->node = node;
           sm->rejected = rejected + (pass ? 1 : 0);

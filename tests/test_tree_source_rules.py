@@ -34,3 +34,12 @@ def test_loads_from_tensor_memory_are_the_whole_warps():
         assert "continue;" not in b and "break;" not in b, b
         if re.search(r"\bif \(", b):
             assert b.rstrip().endswith("__syncwarp();"), b
+
+
+def test_the_walks_words_are_written_behind_their_readers():
+    """The walking warp's lanes read the last round's words (A among them); the lane that writes the next round's waits for them."""
+    code = re.sub(r"//.*", "", open(os.path.join(CSRC, "tree_verify.cu")).read())
+    writes = [m.start() for m in re.finditer(r"if \(tid == 0\) \{\s*sm->node = ", code)]
+    assert len(writes) == 1
+    for w in writes:
+        assert code[:w].rstrip().endswith("__syncwarp();")
