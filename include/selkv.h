@@ -456,8 +456,9 @@ SELKV_API selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv
  *   RAMP        the same with k_f = 1 - (f - i0) / (i1 - i0) clamped, i0 = max(0, floor(c(high))),
  *               i1 = min(rot_dim - 1, ceil(c(low))), c(n) = rot_dim ln(original / (2 pi n)) / (2 ln theta)
  *               (i1 - i0 at least 0.001).
- * Angles are taken in turns in 64-bit fixed point (their wrap is the reduction): right to 2^-33 turns for every
- * 32-bit position; sine, cosine and products in fp32, one rounding to the dtype at the end.
+ * Angles are taken in turns in 64-bit fixed point (their wrap is the reduction): right to 2^-31 turns for every
+ * 32-bit position (with factor and theta such that a pair turns less than 2^19 times a position), then rounded to fp32 (2^-26
+ * turns); sine, cosine and products in fp32, one rounding to the dtype at the end.
  * ------------------------------------------------------------------------------------- */
 typedef enum selkv_rope_scale {
   SELKV_ROPE_SCALE_NONE = 0,

@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "quant.cuh"
+#include "rope_turns.h"
 #include "selkv_internal.cuh"
 #include "tree.cuh"
 
@@ -228,25 +229,6 @@ bool tree_rows_ok(const selkv_shape& s) {
 constexpr int32_t kMaxVocab = 1 << 20;
 bool tree_ok(const selkv_tree* t) {
   return t != nullptr && t->tokens >= 1 && t->tokens <= SELKV_MAX_TREE && aligned(t->parents, 4) && aligned(t->counts, 4);
-}
-
-constexpr double kTwoPi = 6.283185307179586476925;
-
-// Radians per position of pair f.
-double rope_frequency(int f, int rot, double theta, const selkv_rope_scaling* s) {
-  const double w = std::pow(theta, -2.0 * f / rot);
-  if (s == nullptr || s->kind == SELKV_ROPE_SCALE_NONE) return w;
-  if (s->kind == SELKV_ROPE_SCALE_LINEAR) return w / s->factor;
-  double keep;
-  if (s->kind == SELKV_ROPE_SCALE_WAVELENGTH) {
-    keep = (s->original * w / kTwoPi - s->low) / (s->high - s->low);
-  } else {
-    auto pair_of = [&](double turns) { return rot * std::log(s->original / (kTwoPi * turns)) / (2.0 * std::log(theta)); };
-    const double i0 = std::fmax(0.0, std::floor(pair_of(s->high))), i1 = std::fmin(rot - 1.0, std::ceil(pair_of(s->low)));
-    keep = 1.0 - (f - i0) / std::fmax(i1 - i0, 0.001);
-  }
-  keep = std::fmin(1.0, std::fmax(0.0, keep));
-  return keep * w + (1.0 - keep) * w / s->factor;
 }
 
 template <typename T>
@@ -754,11 +736,9 @@ selkv_status selkv_rotary_init(selkv_rotary* plan, int32_t rot_dim, int32_t layo
     else if (c.kind == SELKV_ROPE_SCALE_RAMP && c.factor > 1.0) amplitude = 0.1 * std::log(c.factor) + 1.0;
   }
   uint64_t turns[SELKV_ROTARY_MAX_DIM / 2] = {};
-  for (int f = 0; f < rot_dim / 2; ++f) {
-    const double t = rope_frequency(f, rot_dim, theta, scaling) / kTwoPi;
-    if (!std::isfinite(t)) return SELKV_ERR_INVALID_ARG;
-    turns[f] = (uint64_t)std::ldexp(t - std::floor(t), 64);  // whole turns fall away (below 1: within 64 bits)
-  }
+  const Wide log_theta = wide_log(theta);
+  for (int f = 0; f < rot_dim / 2; ++f)
+    if (!rope_turns(f, rot_dim, log_theta, scaling, &turns[f])) return SELKV_ERR_INVALID_ARG;
   plan->layout = layout;
   plan->rot_dim = rot_dim;
   plan->amplitude = (float)amplitude;

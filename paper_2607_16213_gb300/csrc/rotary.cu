@@ -2,7 +2,8 @@
 //
 // Pair f of a row at position p turns by p w_f.  The angle in turns is p times the plan's 64-bit fraction of a
 // turn per position, and the product's wrap modulo 2^64 takes whole turns off exactly: its upper half is the angle in
-// [-1/2, 1/2) turns, right to 2^-33, for any 32-bit position, without 64-bit floating point (which this GPU has little of).
+// [-1/2, 1/2) turns, right to 2^-31 for any 32-bit position (the plan's fraction to 2^-65, and what is cut off), without 64-bit
+// floating point (which this GPU has little of).  The sine's argument is that in fp32: right to 2^-26 turns.
 //
 // Bound by memory: each element is read and written once (16384 tokens x 40 heads, d 128, bf16: 56 us, 88% of the copy rate; 8
 // tokens: 3.3, a launch's latency).  A thread has the same pairs of one token in all heads of its
