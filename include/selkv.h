@@ -566,9 +566,11 @@ SELKV_API selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tre
  * accepted  [B] int32 output: tokens of the path, token 0 among them (0 for a sequence without tokens).
  * path      [B][T] int32 output: their indices in order, -1 behind them.
  * next_token  [B] int32 output (-1 for a sequence without tokens).
- * Tests are held in 64-bit fixed point (units of 2^-62), sums to 47 bits or more, added in one order: results are the
- * same in every run, and a draw is off only for a number within 2^-47 of a border between two tokens.  A probability that is NaN, negative or at least 2 counts as 0, a token outside the vocabulary is never accepted,
- * a uniform outside [0, 1) is clamped (NaN: 0); each sets SELKV_DEVERR_VALUE where the call meets it.
+ * Tests are held in 64-bit fixed point (units of 2^-62), sums to 42 bits or more, added in one order: results are the
+ * same in every run.  A draw is off only for a number within 2^-42 of a border between two tokens, and a draw or test after k
+ * rejections of drawn drafts that leave a mass of m only for one within 2^-42 (1 + k / m).  A probability that is NaN,
+ * negative or at least 2 counts as 0 (-0 is 0), a token outside the vocabulary is never accepted, a uniform
+ * outside [0, 1) is clamped (NaN: 0); each sets SELKV_DEVERR_VALUE where the call meets it.
  * batch 1 .. SELKV_MAX_BATCH, vocab 1 .. 2^20.  Errors: SELKV_ERR_INVALID_ARG for a NULL or misaligned tensor
  * (draft may be NULL) or a size out of range; SELKV_ERR_WORKSPACE as elsewhere. */
 SELKV_API size_t selkv_tree_verify_workspace_size(int32_t batch, int32_t tokens, int32_t vocab);

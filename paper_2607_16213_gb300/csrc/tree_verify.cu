@@ -7,11 +7,17 @@
 //
 // Tests and sums are held in 64-bit fixed point, units of 2^-62.  A pass adds up each thread's few weights as an fp32 number and its
 // error (an exact difference of three operations and an exact sum of six, where a 64-bit sum took 70 instructions an entry)
-// and goes on in fixed point from there: 47 bits or more.  So the token that a given number draws does not depend on
-// how the vocabulary is split, but for borders within 2^-47 of it.  (Sums in fp32 would move the borders between tokens by
-// 2^-24 of the whole: one draw in a hundred over a flat vocabulary of 128k.)  After k rejections the weights are
-// max(p - A q, 0) with A the sum of the masses that they were taken with (max(max(x, 0) - y, 0) is max(x - y, 0) for
-// y >= 0), so a pass costs the same however many there were.
+// and goes on in fixed point from there.  So the token that a given number draws depends on how the vocabulary is split for
+// borders right beside it alone.  (Sums in fp32 would move the borders between tokens by 2^-24 of the whole: one draw in a hundred
+// over a flat vocabulary of 128k.)  After k rejections the weights are max(p - A q, 0) with A the sum of the masses that they were
+// taken with (max(max(x, 0) - y, 0) is max(x - y, 0) for y >= 0), so a pass costs the same however many there were.
+//
+// How far a border may be off, u = 2^-24.  Eight entries in a Pair: errors of up to u of the sum each, whose own sum is rounded to u
+// of itself: at most (2 + .. + 8 + 8) u^2 = 43 u^2 of the sum; whole units: 1.5 x 2^-62 an eight, 2^-44.4 for 2^20 entries.  Together
+// below 2^-42.2 of the mass m.  From the second rejection on, an entry p - A q cancels: A as two numbers, l and e rounded,
+// 2^-45.4 of p, so that of the whole.  A takes on the errors of the masses in it, but not more (a larger A leaves a smaller mass,
+// by less).  So after k rejections sums and tests are right to 2^-42 (m + k), and in parts of m, as the numbers count, to
+// 2^-42 (1 + k / m).  Met, for 8192 entries and two rejections: 2^-48.7 of m = 0.0023, 2^-38.5 of m = 0.00023.
 //
 // 1 x 32000 entries, 8 tokens: 8 us on the GPU, latencies (tests, pass, draw).  64 x 128000, 16 tokens: 41 us where the rows of the
 // 1.5 passes a sequence takes would need 14: latencies, and sequences with up to four passes (about 25 instructions

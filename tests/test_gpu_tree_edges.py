@@ -2,6 +2,7 @@
 import decimal
 import math
 from decimal import Decimal as D
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -71,3 +72,73 @@ def test_tree_verify_takes_negative_zeros_for_zeros(V, drawn):
     got = run_verify(tokens, parents, neg[0], neg[1], neg[2] if drawn else None, None, ws)
     assert all(np.array_equal(x, y) for x, y in zip(got, want))
     assert ws.errors() == 0
+
+
+def left_of(p, q, tokens):
+    """The weights after the rejection of each of `tokens` in turn, without error."""
+    P = [int(x * 2.0 ** 160) for x in p.astype(np.float64)]
+    if q is None:
+        for x in tokens:
+            P[x] = 0
+        return [Fraction(x, 2 ** 160) for x in P]
+    Q = [int(x * 2.0 ** 160) for x in q.astype(np.float64)]
+    A, r = Fraction(0), [Fraction(x, 2 ** 160) for x in P]
+    M = Fraction(1)
+    for _ in tokens:
+        A += M
+        num, den = A.numerator, A.denominator
+        whole = [max(a * den - num * b, 0) for a, b in zip(P, Q)]
+        M = Fraction(sum(whole), den * 2 ** 160)
+        r = [Fraction(x, den * 2 ** 160) for x in whole]
+    return r
+
+
+def bring_border(p, q, tokens, u0, k, sign):
+    """Adds to entries 0 to 2 (without weight in q, each finer than the one before) until the running sum of some entry lies 1 to 2
+    times the documented distance, 2^-42 (1 + k / mass left) of the whole, from u0 of the whole, above it or below (`sign`).
+    Returns the token that u0 draws."""
+    for step in range(24):
+        r = left_of(p, q, tokens)
+        Z = sum(r)
+        at, c, j, below = Fraction(float(u0)) * Z, Fraction(0), 0, Fraction(0)
+        away = Fraction(2) ** -42 * (Z + k) * Fraction(3, 2)
+        for i, x in enumerate(r):  # the last border that is not far above
+            c += x
+            if c - at > 4 * away:
+                break
+            if x > 0:
+                j, below = i, c
+        gap = sign * away - (below - at)
+        if abs(gap) < away / 3:
+            return j if sign > 0 else next(i for i in range(j + 1, len(r)) if r[i] > 0)
+        knob = min(2, step // 6)
+        move = float(gap / (1 - Fraction(float(u0))))
+        p[knob] = np.float32(float(p[knob]) + (move if knob == 2 else 0.9 * max(0.0, move)))  # (the rest is left to the finer ones)
+        assert p[knob] >= 0
+    raise AssertionError("the border was not brought there")
+
+
+@pytest.mark.parametrize("drawn,k", [(True, 0), (True, 1), (True, 2), (True, 3), (False, 2)])
+@pytest.mark.parametrize("V,eps", [(2000, 0.3), (8192, 0.01), (8191, 0.0005)])
+def test_tree_verify_draws_near_a_border(drawn, k, V, eps):
+    """A draft that is close to its target leaves little mass: borders between tokens are right to 2^-42 (1 + k / mass) of it."""
+    rng = np.random.default_rng(V + k)
+    cases = []
+    for u0, sign in ((0.5, 1), (0.5, -1), (0.75, 1), (0.2501, -1)):
+        q = 0.5 + rng.random(V)
+        p = np.abs(q * (1 + eps * rng.normal(size=V)))
+        p, q = (p / p.sum()).astype(np.float32), (q / q.sum()).astype(np.float32)
+        q[:3] = 0
+        p[:3] = 0
+        tokens = [int(x) for x in np.argsort(p[3:] / q[3:])[:k] + 3]
+        u0 = np.float32(u0)
+        want = bring_border(p, q if drawn else None, tokens, u0, k if drawn else 0, sign)
+        cases.append((p, q, tokens, u0, want))
+    T = k + 1
+    target, draft = (np.stack([np.stack([c[i]] * T) for c in cases]) for i in (0, 1))
+    tok = np.array([[0] + c[2] for c in cases])
+    u = np.full((len(cases), T), 1 - 2.0 ** -24, dtype=np.float32)
+    u[:, 0] = [c[3] for c in cases]
+    got = run_verify(tok, np.array([[-1] + [0] * k] * len(cases)), u, target, draft if drawn else None)
+    assert list(got[0]) == [1] * len(cases)
+    assert list(got[2]) == [c[4] for c in cases]
