@@ -562,7 +562,8 @@ SELKV_API selkv_status selkv_tree_attn(const selkv_shape* shape, const selkv_tre
  * tokens    [B][T] int32 device, in [0, vocab) (token 0's is not read).
  * uniforms  [B][T] fp32 device, in [0, 1): entry t > 0 decides on token t, entry 0 draws the next token.
  * target    [B][T][vocab] fp32 device: row t the probabilities of what follows token t; draft the same or NULL.  A row's
- *           sum is 1 up to rounding; a sum of 4 or more sets SELKV_DEVERR_VALUE, and any token may follow.
+ *           sum is 1 up to rounding; a sum of 4 or more sets SELKV_DEVERR_VALUE, and any token may follow; so does a row
+ *           without mass that the next token is drawn from (vocab - 1 follows).
  * accepted  [B] int32 output: tokens of the path, token 0 among them (0 for a sequence without tokens).
  * path      [B][T] int32 output: their indices in order, -1 behind them.
  * next_token  [B] int32 output (-1 for a sequence without tokens).

@@ -433,7 +433,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_verify_kernel(VerifyArgs a, 
     cluster_arrive();
     cluster_wait();
     // (the first warp's from here on: it knows the sum)
-    if (tid < 32 && Z == 0) bad = true;
+    // (a row without mass is none; one whose picked drafts took all that its sum, a rounding below 1, had is)
+    if (tid < 32 && Z == 0) bad = bad || M == kOne;
     else if (tid < 32 && at >= below && at - below < own) {
       const int spans = (hi - lo + kSpan - 1) / kSpan;
       u64 rest = at - below;  // mass before the entry

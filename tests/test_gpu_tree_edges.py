@@ -142,3 +142,27 @@ def test_tree_verify_draws_near_a_border(drawn, k, V, eps):
     got = run_verify(tok, np.array([[-1] + [0] * k] * len(cases)), u, target, draft if drawn else None)
     assert list(got[0]) == [1] * len(cases)
     assert list(got[2]) == [c[4] for c in cases]
+
+
+@pytest.mark.parametrize("V", [2, 300, 5000])
+def test_tree_verify_rows_that_are_left_without_mass(V):
+    """Picked drafts that are all that a row holds, each rejected: the row's sum is a rounding below 1, so nothing is wrong with it
+    and the last token follows.  A row that never had mass is reported."""
+    p = np.zeros((1, 3, V), dtype=np.float32)
+    p[:, :, 0], p[:, :, 1] = 0.3, np.float32(0.7) - np.float32(2.0 ** -22)
+    tokens, parents = np.array([[0, 0, 1]]), np.array([[-1, 0, 0]])
+    u = np.array([[0.5, 0.999, 1 - 2.0 ** -24]], dtype=np.float32)
+    ws = api.Workspace(256)
+    got = run_verify(tokens, parents, u, p, None, None, ws)
+    check_verify(got, tokens, parents, u, p, None)
+    assert got[2][0] == V - 1 and ws.errors() == 0
+    for draft in (None, p):
+        got = run_verify(tokens, parents, u, np.zeros_like(p), draft, None, ws)
+        assert got[0][0] == 1 and got[2][0] == V - 1 and ws.errors() == S.SELKV_DEVERR_VALUE
+    # a row without mass that the walk leaves by a child is not drawn from
+    q = p.copy()
+    q[0, 0] = 0
+    q[0, 0, 1] = 1.0
+    q[0, 1] = 0
+    got = run_verify(tokens, np.array([[-1, 0, 0]]), u, q, None, None, ws)
+    assert list(got[1][0]) == [0, 2, -1] and ws.errors() == 0
