@@ -4,6 +4,7 @@
 
 #include <cudaTypedefs.h>
 
+#include "map_store.h"
 #include "ptx.cuh"
 #include "selkv_internal.cuh"
 
@@ -27,32 +28,17 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
 }  // namespace
 
 // Encodings are kept by (base, rows, d, box rows): the same buffers come back call after call (a decode step per
-// layer), and a map depends on nothing else.  A place per hash, taken by the last one that asked.
+// layer), and a map depends on nothing else.
 namespace {
-struct MapEntry {
-  const void* base;
-  uint64_t rows;
-  int d, box;
-  CUtensorMap map;
-};
-constexpr int kMapCache = 2048;
 std::mutex g_map_mu;
-MapEntry g_maps[kMapCache];
-
-MapEntry& place_of(const void* base, uint64_t rows, int d, int box_rows) {
-  uint64_t h = reinterpret_cast<uintptr_t>(base) >> 4;
-  h = (h ^ rows * 31u ^ (uint64_t)(d * 257 + box_rows) * 7919u) * 0x9E3779B97F4A7C15ull;
-  return g_maps[h >> 53];
-}
-static_assert(kMapCache == 1 << 11, "the hash's upper 11 bits");
+MapStore<CUtensorMap, 2048> g_maps;
 }  // namespace
 
 bool encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, int box_rows) {
-  MapEntry& e = place_of(base, rows, d, box_rows);
   {
     std::lock_guard<std::mutex> lock(g_map_mu);
-    if (base != nullptr && e.base == base && e.rows == rows && e.d == d && e.box == box_rows) {
-      *map = e.map;
+    if (const CUtensorMap* kept = g_maps.find(base, rows, d, box_rows)) {
+      *map = *kept;
       return true;
     }
   }
@@ -67,11 +53,7 @@ bool encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, 
          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return false;
   std::lock_guard<std::mutex> lock(g_map_mu);
-  e.base = base;
-  e.rows = rows;
-  e.d = d;
-  e.box = box_rows;
-  e.map = *map;
+  g_maps.put(base, rows, d, box_rows, *map);
   return true;
 }
 
