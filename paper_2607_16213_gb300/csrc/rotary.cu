@@ -44,7 +44,8 @@ struct Chunk {
 template <typename T, int VEC, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const __grid_constant__ RotaryArgs a, int nheads) {
   const int half = a.rot / 2, pairs = half / VEC, items = pairs + (a.D - a.rot) / (2 * VEC), tokens = kThreads / items;
-  const int ti = threadIdx.x / items, it = threadIdx.x - ti * items, t = blockIdx.x * tokens + ti, b = blockIdx.z;
+  const int ti = threadIdx.x / items, it = threadIdx.x - ti * items, b = blockIdx.z;
+  const int64_t t = (int64_t)blockIdx.x * tokens + ti;  // (the last CTA's may pass 32 bits)
   if (ti >= tokens || t >= a.T) return;
   const bool turns = it < pairs;
   float c[VEC], s[VEC];
@@ -100,11 +101,11 @@ template <typename T, int VEC>
 cudaError_t launch(const RotaryArgs& a, cudaStream_t s) {
   const int heads = (a.q != nullptr ? a.Hq : 0) + (a.k != nullptr ? a.Hkv : 0);
   const int items = a.rot / (2 * VEC) + (a.D - a.rot) / (2 * VEC), tokens = kThreads / items;
-  const int64_t tiles = (int64_t)((a.T + tokens - 1) / tokens) * a.B;
+  const int64_t across = ((int64_t)a.T + tokens - 1) / tokens, tiles = across * a.B;
   // many heads share a thread's angles, but not so many that SMs stay empty
   int each = kMostHeads;
   while (each > kFewestHeads && tiles * ((heads + each - 1) / each) < 4 * kPlanSMs) each /= 2;
-  const dim3 grid((unsigned)((a.T + tokens - 1) / tokens), (unsigned)((heads + each - 1) / each), (unsigned)a.B);
+  const dim3 grid((unsigned)across, (unsigned)((heads + each - 1) / each), (unsigned)a.B);
   if (a.layout == SELKV_ROPE_HALF) rotary_kernel<T, VEC, true><<<grid, kThreads, 0, s>>>(a, each);
   else rotary_kernel<T, VEC, false><<<grid, kThreads, 0, s>>>(a, each);
   return cudaGetLastError();
