@@ -736,9 +736,7 @@ selkv_status selkv_rotary_init(selkv_rotary* plan, int32_t rot_dim, int32_t layo
     else if (c.kind == SELKV_ROPE_SCALE_RAMP && c.factor > 1.0) amplitude = 0.1 * std::log(c.factor) + 1.0;
   }
   uint64_t turns[SELKV_ROTARY_MAX_DIM / 2] = {};
-  const Wide log_theta = wide_log(theta);
-  for (int f = 0; f < rot_dim / 2; ++f)
-    if (!rope_turns(f, rot_dim, log_theta, scaling, &turns[f])) return SELKV_ERR_INVALID_ARG;
+  if (!rope_turns(rot_dim, theta, scaling, turns)) return SELKV_ERR_INVALID_ARG;
   plan->layout = layout;
   plan->rot_dim = rot_dim;
   plan->amplitude = (float)amplitude;

@@ -63,33 +63,38 @@ inline Wide wide_log(double x) {
   return y + kWideLn2 * Wide{(double)e, 0.0};
 }
 
-// Pair f's turns a position, modulo one and in units of 2^-64 (rounded; right to that up to 2^29 turns a position); false where
-// they are no number.  `log_theta` is theta's.
-inline bool rope_turns(int f, int rot, Wide log_theta, const selkv_rope_scaling* s, uint64_t* turns) {
-  const Wide w = wide_exp(-(Wide{2.0 * f, 0.0} / Wide{(double)rot, 0.0} * log_theta));
-  Wide t = w / kWideTwoPi;
-  if (s != nullptr && s->kind != SELKV_ROPE_SCALE_NONE) {
-    Wide keep{0.0, 0.0};
-    if (s->kind == SELKV_ROPE_SCALE_WAVELENGTH) {
-      keep = (t * Wide{(double)s->original, 0.0} - Wide{s->low, 0.0}) / (Wide{s->high, 0.0} - Wide{s->low, 0.0});
-    } else if (s->kind == SELKV_ROPE_SCALE_RAMP) {
-      // the pair that turns n times over the original context
-      auto pair_of = [&](double n) {
-        return Wide{(double)rot, 0.0} * (wide_log((double)s->original) - wide_log(kWideTwoPi.hi) - Wide{kWideTwoPi.lo / kWideTwoPi.hi, 0.0} -
-                                         wide_log(n)) / (log_theta + log_theta);
-      };
-      const double i0 = std::fmax(0.0, wide_floor(pair_of(s->high)).hi), i1 = std::fmin(rot - 1.0, -wide_floor(-pair_of(s->low)).hi);
-      keep = Wide{1.0, 0.0} - Wide{f - i0, 0.0} / Wide{std::fmax(i1 - i0, 0.001), 0.0};
-    }
-    const Wide none{0.0, 0.0}, all{1.0, 0.0};
-    keep = keep < none ? none : all < keep ? all : keep;
-    t = keep * t + (all - keep) * t / Wide{s->factor, 0.0};
+// The pairs' turns a position, modulo one and in units of 2^-64, into turns[0 .. rot / 2 - 1] (rounded; right to that where a pair
+// turns less than 2^19 times a position); false where one is no number.  w_f is the power of w_1: 63 products leave 2^-88.
+inline bool rope_turns(int rot, double theta, const selkv_rope_scaling* s, uint64_t* turns) {
+  const int kind = s != nullptr ? s->kind : SELKV_ROPE_SCALE_NONE;
+  const Wide none{0.0, 0.0}, all{1.0, 0.0}, log_theta = wide_log(theta);
+  const Wide step = wide_exp(-(Wide{2.0, 0.0} / Wide{(double)rot, 0.0} * log_theta));
+  double i0 = 0.0, i1 = 0.0;
+  if (kind == SELKV_ROPE_SCALE_RAMP) {
+    const Wide log_span = wide_log((double)s->original) - wide_log(kWideTwoPi.hi) - Wide{kWideTwoPi.lo / kWideTwoPi.hi, 0.0};
+    // the pair that turns n times over the original context
+    auto pair_of = [&](double n) { return Wide{(double)rot, 0.0} * (log_span - wide_log(n)) / (log_theta + log_theta); };
+    i0 = std::fmax(0.0, wide_floor(pair_of(s->high)).hi);
+    i1 = std::fmin(rot - 1.0, -wide_floor(-pair_of(s->low)).hi);
   }
-  if (!std::isfinite(t.hi) || !std::isfinite(t.lo)) return false;
-  t = t - wide_floor(t);
-  const double high = std::ldexp(t.hi, 64), whole = std::floor(high);
-  const double rest = std::floor((high - whole) + std::ldexp(t.lo, 64) + 0.5);  // (a few thousand at most)
-  *turns = (whole < 0x1p64 ? (uint64_t)whole : 0u) + (uint64_t)(int64_t)rest;
+  Wide w = all;
+  for (int f = 0; f < rot / 2; ++f, w = w * step) {
+    Wide t = w / kWideTwoPi;
+    if (kind != SELKV_ROPE_SCALE_NONE) {
+      Wide keep = none;
+      if (kind == SELKV_ROPE_SCALE_WAVELENGTH)
+        keep = (t * Wide{(double)s->original, 0.0} - Wide{s->low, 0.0}) / (Wide{s->high, 0.0} - Wide{s->low, 0.0});
+      else if (kind == SELKV_ROPE_SCALE_RAMP)
+        keep = all - Wide{f - i0, 0.0} / Wide{std::fmax(i1 - i0, 0.001), 0.0};
+      keep = keep < none ? none : all < keep ? all : keep;
+      t = keep * t + (all - keep) * t / Wide{s->factor, 0.0};
+    }
+    if (!std::isfinite(t.hi) || !std::isfinite(t.lo)) return false;
+    t = t - wide_floor(t);
+    const double high = std::ldexp(t.hi, 64), whole = std::floor(high);
+    const double rest = std::floor((high - whole) + std::ldexp(t.lo, 64) + 0.5);  // (a few thousand at most)
+    turns[f] = (whole < 0x1p64 ? (uint64_t)whole : 0u) + (uint64_t)(int64_t)rest;
+  }
   return true;
 }
 
