@@ -45,8 +45,8 @@ template <typename T, int VEC, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const __grid_constant__ RotaryArgs a, int nheads) {
   const int half = a.rot / 2, pairs = half / VEC, items = pairs + (a.D - a.rot) / (2 * VEC), tokens = kThreads / items;
   const int ti = threadIdx.x / items, it = threadIdx.x - ti * items, b = blockIdx.z;
-  const int64_t t = (int64_t)blockIdx.x * tokens + ti;  // (the last CTA's may pass 32 bits)
-  if (ti >= tokens || t >= a.T) return;
+  const uint32_t t = blockIdx.x * tokens + ti;  // (the last CTA's may pass 2^31)
+  if (ti >= tokens || t >= (uint32_t)a.T) return;
   const bool turns = it < pairs;
   float c[VEC], s[VEC];
   if (turns) {

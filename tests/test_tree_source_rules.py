@@ -45,8 +45,8 @@ def test_the_walks_words_are_written_behind_their_readers():
         assert code[:w].rstrip().endswith("__syncwarp();")
 
 
-def test_rotary_counts_tokens_in_64_bits():
-    """Up to 2^31 - 1 tokens: the last CTA's places behind them, and their number rounded up, do not fit 32 bits."""
+def test_rotary_counts_tokens_past_an_int():
+    """Up to 2^31 - 1 tokens: the last CTA's places behind them, and their number rounded up, do not fit an int."""
     code = re.sub(r"//.*", "", open(os.path.join(CSRC, "rotary.cu")).read())
-    assert re.findall(r"(\S+) \* tokens", code) == ["(int64_t)blockIdx.x"]
+    assert re.findall(r"(\S+ \S+) = blockIdx.x \* tokens", code) == ["uint32_t t"] and "t >= (uint32_t)a.T" in code
     assert re.findall(r"(\S+) \+ tokens - 1", code) == ["((int64_t)a.T"]
