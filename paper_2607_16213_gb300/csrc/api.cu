@@ -226,7 +226,6 @@ TreePlan plan_tree(const selkv_shape& s, int tokens) {
 bool tree_rows_ok(const selkv_shape& s) {
   return (s.head_dim == 64 || s.head_dim == 128) && (int64_t)s.batch * s.num_kv_heads * s.m_cap < (int64_t)1 << 31;
 }
-constexpr int32_t kMaxVocab = 1 << 20;
 bool tree_ok(const selkv_tree* t) {
   return t != nullptr && t->tokens >= 1 && t->tokens <= SELKV_MAX_TREE && aligned(t->parents, 4) && aligned(t->counts, 4);
 }

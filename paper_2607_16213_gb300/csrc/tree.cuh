@@ -271,6 +271,7 @@ struct RotaryArgs {
 };
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t s);
 
+constexpr int kMaxVocab = 1 << 20;  // (the sums of a CTA's spans have places in shared memory for that many)
 struct VerifyArgs {
   int B, T, V;
   const int32_t* parents;

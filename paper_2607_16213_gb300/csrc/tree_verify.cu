@@ -32,7 +32,6 @@ typedef unsigned long long u64;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kSpan = 256;              // entries of a warp's step: a sum is kept for each
-constexpr int kMaxVocab = 1 << 20;
 constexpr u64 kOne = 1ull << 62;
 
 // a * b in units of 2^-62, for a < 2^64 and b < 2^62.

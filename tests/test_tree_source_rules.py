@@ -50,3 +50,9 @@ def test_rotary_counts_tokens_past_an_int():
     code = re.sub(r"//.*", "", open(os.path.join(CSRC, "rotary.cu")).read())
     assert re.findall(r"(\S+ \S+) = blockIdx.x \* tokens", code) == ["uint32_t t"] and "t >= (uint32_t)a.T" in code
     assert re.findall(r"(\S+) \+ tokens - 1", code) == ["((int64_t)a.T"]
+
+
+def test_the_largest_vocabulary_is_said_once():
+    """The check of the argument and the shared memory that it keeps from overflowing go by one number."""
+    said = [name for name in sorted(os.listdir(CSRC)) for _ in re.findall(r"\bkMaxVocab =", open(os.path.join(CSRC, name)).read())]
+    assert said == ["tree.cuh"]
