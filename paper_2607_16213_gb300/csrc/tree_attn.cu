@@ -27,7 +27,7 @@ __device__ __forceinline__ void put_out(const TreeArgs& a, int b, int kv, int r,
 // The products run on the FMA units: R rows cost 4 R d operations per key for 8 d bytes, so above about 20 rows
 // a KV head the arithmetic bounds it, below the loads.  2 x 1000 rows x 2 heads, d 64, 7 tokens: 13.9 us a pass on the GPU, the join
 // 3 us of it: latency (list, tile, statistics, partials); 16000 rows: 37.9.
-template <typename T, int D, int RPT>
+template <int D, int RPT>
 __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
   constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;
   constexpr int LD = D + 4, PLD = KEYS + 4;  // (padded: 16 rows' float4 in different banks)
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
     const int cache_tiles = (p.L + KEYS - 1) / KEYS;
     const int row0 = p.blk * RT, rows = min(RT, a.R - row0);
     __syncthreads();  // the last piece's rows are read
-    const T* q = static_cast<const T*>(a.q) + (((size_t)p.b * a.Hq + p.kv * a.G) * a.T + row0) * D;
+    const float* q = static_cast<const float*>(a.q) + (((size_t)p.b * a.Hq + p.kv * a.G) * a.T + row0) * D;
     for (int i = tid; i < RT * (D / 4); i += kThreads) {
       const int r = i / (D / 4), d = i % (D / 4) * 4;
       float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -75,8 +75,8 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
     for (int t = p.first; t < p.first + p.count; ++t) {
       const bool drafts = t >= cache_tiles;
       const int key0 = (drafts ? t - cache_tiles : t) * KEYS, keys = min(KEYS, (drafts ? p.n : p.L) - key0);
-      const T* kp = static_cast<const T*>(drafts ? a.k_new : a.Kc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
-      const T* vp = static_cast<const T*>(drafts ? a.v_new : a.Vc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
+      const float* kp = static_cast<const float*>(drafts ? a.k_new : a.Kc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
+      const float* vp = static_cast<const float*>(drafts ? a.v_new : a.Vc) + (bk * (drafts ? a.T : a.m_cap) + key0) * D;
       const float* bias = drafts || a.bias == nullptr ? nullptr : a.bias + bk * a.m_cap + key0;
       __syncthreads();  // the last tile is read (and Q is there)
       for (int i = tid; i < KEYS * (D / 4); i += kThreads) {
@@ -117,7 +117,6 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
 #pragma unroll
       for (int i = 0; i < RPT; ++i) {
         float mx = -INFINITY;
-        bool nan = false;
         const uint4 sees = drafts ? seen[tok[i]] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -129,7 +128,6 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
             in = in && ((w >> (key & 31)) & 1u);
           }
           s[i][j] = in ? s[i][j] + b : -INFINITY;
-          nan = nan || s[i][j] != s[i][j];
           mx = fmaxf(mx, s[i][j]);
         }
 #pragma unroll
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
 #pragma unroll
           for (int e = 0; e < NE; ++e) {
             const float x[4] = {o[i][e * 4] * inv, o[i][e * 4 + 1] * inv, o[i][e * 4 + 2] * inv, o[i][e * 4 + 3] * inv};
-            put_out<T>(a, p.b, p.kv, row0 + r, tx * 4 + 64 * e, x);
+            put_out<float>(a, p.b, p.kv, row0 + r, tx * 4 + 64 * e, x);
           }
         }
       }
@@ -203,12 +201,12 @@ __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
   }
 }
 
-template <typename T, int D, int RPT>
+template <int D, int RPT>
 cudaError_t launch_simt(const TreeArgs& a, int ctas, cudaStream_t s) {
   constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;
   constexpr int fixed = (RT * (D + 4) + KEYS * (D + 4) + KEYS * D + KEYS) * 4 + SELKV_MAX_TREE * 16;
-  if (const cudaError_t e = set_smem_once<tree_simt_kernel<T, D, RPT>>(fixed + tree_list_bytes(SELKV_MAX_BATCH)); e != cudaSuccess) return e;
-  return launch_chained(true, tree_simt_kernel<T, D, RPT>, dim3((unsigned)ctas), dim3(kThreads), (size_t)(fixed + tree_list_bytes(a.B)), s, a);
+  if (const cudaError_t e = set_smem_once<tree_simt_kernel<D, RPT>>(fixed + tree_list_bytes(SELKV_MAX_BATCH)); e != cudaSuccess) return e;
+  return launch_chained(true, tree_simt_kernel<D, RPT>, dim3((unsigned)ctas), dim3(kThreads), (size_t)(fixed + tree_list_bytes(a.B)), s, a);
 }
 
 // ---- joining the pieces of a unit ----------------------------------------------------------
@@ -294,9 +292,9 @@ cudaError_t launch_tree_attn(const TreeArgs& a, cudaStream_t s) {
     return a.D == 128 ? launch_join<__nv_bfloat16, 128>(a, s) : launch_join<__nv_bfloat16, 64>(a, s);
   }
   if (a.R <= 16)
-    e = a.D == 128 ? launch_simt<float, 128, 1>(a, ctas, s) : launch_simt<float, 64, 1>(a, ctas, s);
+    e = a.D == 128 ? launch_simt<128, 1>(a, ctas, s) : launch_simt<64, 1>(a, ctas, s);
   else
-    e = a.D == 128 ? launch_simt<float, 128, 4>(a, ctas, s) : launch_simt<float, 64, 4>(a, ctas, s);
+    e = a.D == 128 ? launch_simt<128, 4>(a, ctas, s) : launch_simt<64, 4>(a, ctas, s);
   if (e != cudaSuccess) return e;
   return a.D == 128 ? launch_join<float, 128>(a, s) : launch_join<float, 64>(a, s);
 }

@@ -11,7 +11,7 @@
 // passes it by more than 8 (a factor of 256, far inside the range of bf16 and fp32): O is rescaled in those tiles alone.
 //
 // Arithmetic per byte is 4 R d / (4 d) = R operations: with up to 256 rows the cache's bytes bound it (281 a byte at the
-// measured peaks).  All CTAs have equal shares of the list of key tiles (tree.cuh).
+// measured peaks).  A CTA takes a piece of a unit, or an equal share of the list of all key tiles (tree.cuh).
 //
 // A pass with the join, 8 KV heads, d 128: 25000 rows and 4 tokens (16 rows a head) 28.4 us, 32 tokens 30.7 (floor 15.2:
 // start, list and the first copies take 4 us, the end and the join 6); 8 x 8192-16384 rows, 25 tokens 73.4 (55); 131072 rows, 64
