@@ -166,3 +166,42 @@ def test_tree_verify_rows_that_are_left_without_mass(V):
     q[0, 1] = 0
     got = run_verify(tokens, np.array([[-1, 0, 0]]), u, q, None, None, ws)
     assert list(got[1][0]) == [0, 2, -1] and ws.errors() == 0
+
+
+# ---- attention ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("hkv,d,cap,lengths,T,counts", [
+    (1, 128, 300, [300], 65, None), (2, 128, 700, [613, 1], 128, [128, 97]), (4, 64, 90, [64, 0, 90], 100, [100, 66, 64]),
+    (8, 64, 3000, [2999], 127, None), (2, 128, 64, [0, 0], 65, [65, 65]), (3, 128, 130, [128, 129, 17], 128, [1, 64, 128])])
+@pytest.mark.parametrize("bias,parents", [("ratio", "tree"), (None, "chain"), ("masked", "forest")])
+def test_tree_attn_one_query_head_and_two_tiles_of_tokens(hkv, d, cap, lengths, T, counts, bias, parents):
+    """bf16, a query head a KV head, 65 to 128 tokens: all rows in one accumulator, and the tokens' own rows in two tiles, which
+    the two chains take each one of or, where they lie in different pieces, one after the other."""
+    c = Case("bf16", len(lengths), hkv, hkv, d, cap, lengths, T, counts, bias=bias, parents=parents)
+    before = torch.full_like(c.q, 7.0)
+    ws = api.Workspace(S.selkv_tree_attn_workspace_size(c.shape, T))
+    out = c.run(out=before.clone(), workspace=ws)
+    c.check(out, before=before)
+    assert ws.errors() == 0
+    assert torch.equal(c.run(out=before.clone(), workspace=ws), out)
+
+
+@pytest.mark.parametrize("hq,hkv,T,cap", [(16, 2, 20, 137), (8, 1, 40, 600), (4, 1, 70, 64), (2, 1, 100, 200), (1, 1, 90, 2000), (8, 2, 96, 30)])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_tree_attn_values_that_are_no_numbers(hq, hkv, T, cap, what):
+    """bf16 with more than 128 query rows, where both accumulators' warps clear the same drafted values that are no numbers, and with
+    two tiles of tokens: such a value reaches the tokens that see it, in its element alone."""
+    for seed in range(4):
+        c = Case("bf16", 2, hq, hkv, 64, cap, [cap, cap // 2], T, None, seed=seed, parents="forest")
+        clean = c.run()
+        rng = np.random.default_rng(seed)
+        sees = [R.ancestors(c.pr[b], T) for b in range(2)]
+        hit = np.zeros((2, hkv, T, 64), dtype=bool)
+        for _ in range(5):
+            b, kv, t, e = int(rng.integers(2)), int(rng.integers(hkv)), int(rng.integers(T)), int(rng.integers(64))
+            c.v[b, kv, t, e] = what
+            hit[b, kv, :, e] |= sees[b][:, t]
+        hit = torch.as_tensor(np.repeat(hit, hq // hkv, axis=1)).cuda()
+        got = c.run()
+        assert torch.equal(got[~hit], clean[~hit])
+        bad = got[hit].float()
+        assert bool((bad.isnan() if math.isnan(what) else bad == what).all())
