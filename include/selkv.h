@@ -82,7 +82,8 @@ typedef enum selkv_select_mode { SELKV_SELECT_SHARED = 0, SELKV_SELECT_PER_HEAD 
  * plain rotary embedding with base rope_theta, frequency f in [0, d/2) turning the pair
  * (k[f], k[f + d/2]) (HALF layout) or (k[2f], k[2f + 1]) (INTERLEAVED layout) by
  * p * rope_theta^(-2f/d).  Positions count from 0 at the first prefill token.  Decode does
- * not rotate: the caller embeds new queries and keys at positions lengths[b], ... . */
+ * not rotate: the caller embeds new queries and keys at positions lengths[b], ... , in the same way (selkv_rotary_apply with
+ * a plan of rot_dim = d without scaling or amplitude). */
 /* Attention compensation (Sec. 3.6): RATIO is SelKV's alpha * ln R (Eq. 6); COUNT is the
  * KeepKV-style alpha * ln(1 + M), M the evicted tokens merged into the kept token (routed to
  * it with g > 0), averaged over KV heads in SHARED mode (alpha = 1: KeepKV's log(1 + M)). */
@@ -459,6 +460,10 @@ SELKV_API selkv_status selkv_decode_attn_q(const selkv_shape* shape, const selkv
  * Angles are taken in turns in 64-bit fixed point (their wrap is the reduction): right to 2^-31 turns for every
  * 32-bit position (with factor and theta such that a pair turns less than 2^19 times a position), then rounded to fp32 (2^-26
  * turns); sine, cosine and products in fp32, one rounding to the dtype at the end.
+ * With params.rope a compression turns the kept keys to their slots by the plain embedding of the whole row.  That goes with a plan
+ * of the same layout and theta = rope_theta (as a float), rot_dim = d, no scaling and amplitude 1, and with no other: keys
+ * that another plan embedded would be turned back by angles that they do not have.  Nothing can check this; keep
+ * SELKV_ROPE_OFF with other plans.
  * ------------------------------------------------------------------------------------- */
 typedef enum selkv_rope_scale {
   SELKV_ROPE_SCALE_NONE = 0,

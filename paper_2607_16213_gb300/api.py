@@ -308,7 +308,8 @@ def rotary_plan(rot_dim: int, theta: float = 10000.0, layout: str = "half", scal
                 factor: float = 1.0, original: int = 0, low: float = 1.0, high: float = 32.0,
                 amplitude: float = 0.0) -> B.selkv_rotary:
     """selkv_rotary_init: the plan of a rotary embedding over the first rot_dim elements of a head, its frequencies
-    scaled for long contexts ("linear", "wavelength" or "ramp") or not (None)."""
+    scaled for long contexts ("linear", "wavelength" or "ramp") or not (None).  With a compression that turns kept keys to their
+    slots (rope on) only the plan that it assumes may go: of the whole head, unscaled, of its layout and theta."""
     if layout not in _LAYOUT or scaling not in _SCALING:
         _bad("rotary_plan: layout is half or interleaved, scaling None, linear, wavelength or ramp")
     plan = B.selkv_rotary()

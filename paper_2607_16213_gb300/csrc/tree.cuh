@@ -33,8 +33,8 @@ struct TreeArgs {
 __host__ __device__ constexpr size_t tree_record_floats(int rows, int D) { return (size_t)rows * (D + 2); }
 
 // Fewest tiles of a piece where a unit is cut: below it a partial's way through memory costs more than the tiles do (bf16, 1000 rows
-// x 8 heads, 8 tokens: 1 tile 13.5 us, 2 12.4, 4 12.8; fp32, 2 x 1000 rows x 2 heads, 7 tokens, where a tile takes longer: 1
-// 13.9, 2 17.0, 4 24.3).
+// x 8 heads, 8 tokens: 1 tile 13.5 us, 2 12.4, 4 12.8; fp32, 2 heads, d 64, 7 tokens, where a tile takes longer: 2 x 1000 rows 1 tile
+// 13.5, 2 16.8, 4 24.2; 2 x 101-201 rows 11.1, 15.2, 20.3; 16000 rows 37.8, 37.8, 41.2).
 constexpr int kTreeTcMinTiles = 2, kTreeSimtMinTiles = 1;
 // What ending one piece and beginning another costs a CTA, in tiles (bf16, 4 x 5000 rows x 8 heads, 8 tokens: 6 or 12 25.6 us, 0
 // 27.5).
@@ -248,7 +248,8 @@ __device__ __forceinline__ void tree_ancestors(const TreeArgs& a, int b, int n, 
 
 constexpr int kTreeTcKeys = 64, kTreeSimtKeys = 64;  // keys of a tile
 // Rows of a block.  Tensor cores: two accumulators of 128 rows where one does not hold them.  CUDA cores: 16 where they hold all (14
-// rows, 2 x 1000 cached ones: blocks of 16 17.0 us, of 64 24.1; 16000: 37.9 and 50.5).
+// rows, 2 heads, d 64: blocks of 16 over 2 x 101-201 cached rows 11.1 us, of 64 14.9; 2 x 1000: 13.5 and 17.8; 16000: 37.8 and
+// 50.3; 2 x 16000: 51.7 and 73.8).
 inline int tree_block_rows(int dtype, int R) {
   if (dtype == SELKV_BF16) return R <= 128 ? 128 : 256;
   return R <= 16 ? 16 : 64;

@@ -25,8 +25,9 @@ __device__ __forceinline__ void put_out(const TreeArgs& a, int b, int kv, int r,
 // fp32: tiles of 64 keys, a thread holds RPT rows x 4 keys of the logits and RPT rows x D / 16 elements of the
 // output; 16 threads share a row, so its statistics and probabilities stay within half a warp.
 // The products run on the FMA units: R rows cost 4 R d operations per key for 8 d bytes, so above about 20 rows
-// a KV head the arithmetic bounds it, below the loads.  2 x 1000 rows x 2 heads, d 64, 7 tokens: 13.9 us a pass on the GPU, the join
-// 3 us of it: latency (list, tile, statistics, partials); 16000 rows: 37.9.
+// a KV head the arithmetic bounds it, below the loads.  2 heads, d 64, 7 tokens, a pass on the GPU: 2 x 101-201 rows 11.1 us, 2 x 1000
+// 13.5, the join 3 us of it: latency (list, tile, statistics, partials); 16000 rows 37.8, 2 x 16000 51.7 (no copy is under way
+// while a tile is worked on).
 template <int D, int RPT>
 __global__ __launch_bounds__(kThreads) void tree_simt_kernel(TreeArgs a) {
   constexpr int RT = RPT * 16, KEYS = kTreeSimtKeys;

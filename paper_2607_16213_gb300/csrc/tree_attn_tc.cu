@@ -13,10 +13,10 @@
 // Arithmetic per byte is 4 R d / (4 d) = R operations: with up to 256 rows the cache's bytes bound it (281 a byte at the
 // measured peaks).  A CTA takes a piece of a unit, or an equal share of the list of all key tiles (tree.cuh).
 //
-// A pass with the join, 8 KV heads, d 128: 25000 rows and 4 tokens (16 rows a head) 28.4 us, 32 tokens 30.7 (floor 15.2:
-// start, list and the first copies take 4 us, the end and the join 6); 8 x 8192-16384 rows, 25 tokens 73.4 (55); 131072 rows, 64
+// A pass with the join, 8 KV heads, d 128: 25000 rows and 4 tokens (16 rows a head) 28.7 us, 32 tokens 30.7 (floor 15.2:
+// start, list and the first copies take 4 us, the end and the join 6); 8 x 8192-16384 rows, 25 tokens 73.9 (55); 131072 rows, 64
 // tokens 128 (79: the chain from S over the softmax to P V takes 2100 cycles a tile of 64 keys, its copies 1400); 64 x
-// 410-819 rows, 9 tokens 71 (25: a CTA goes through 3.4 units, and what is run once a unit, masks, the rows' end, the next
+// 410-819 rows, 9 tokens 72 (25: a CTA goes through 3.4 units, and what is run once a unit, masks, the rows' end, the next
 // piece's start, waits for its instructions).
 #include "tree.cuh"
 

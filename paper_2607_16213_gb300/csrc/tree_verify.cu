@@ -19,7 +19,7 @@
 // by less).  So after k rejections sums and tests are right to 2^-42 (m + k), and in parts of m, as the numbers count, to
 // 2^-42 (1 + k / m).  Met, for 8192 entries and two rejections: 2^-48.7 of m = 0.0023, 2^-38.5 of m = 0.00023.
 //
-// 1 x 32000 entries, 8 tokens: 8 us on the GPU, latencies (tests, pass, draw).  64 x 128000, 16 tokens: 41 us where the rows of the
+// 1 x 32000 entries, 8 tokens: 8.7 us on the GPU, latencies (tests, pass, draw).  64 x 128000, 16 tokens: 41 us where the rows of the
 // 1.5 passes a sequence takes would need 14: latencies, and sequences with up to four passes (about 25 instructions
 // an entry and pass: 8 us of all issue slots).
 #include "tree.cuh"
