@@ -205,3 +205,47 @@ def test_tree_attn_values_that_are_no_numbers(hq, hkv, T, cap, what):
         assert torch.equal(got[~hit], clean[~hit])
         bad = got[hit].float()
         assert bool((bad.isnan() if math.isnan(what) else bad == what).all())
+
+
+# ---- offsets past 32 bits -----------------------------------------------------------------------
+def test_rotary_rows_past_32_bits():
+    """A prompt whose last rows begin past 2^31 elements: to the bit what a call over those rows alone gives."""
+    T, n = 2 ** 24 + 1001, 900
+    shape, plan = api.make_shape("bf16", 1, 1, 1, 128, 8, 64, 64), api.rotary_plan(128)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[None]
+    k = torch.zeros((1, 1, T, 128), dtype=torch.bfloat16, device="cuda")
+    k[:, :, -n:] = torch.randn((1, 1, n, 128), generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+    want = api.rotary(shape, plan, pos[:, -n:].contiguous(), k=k[:, :, -n:].contiguous())[1]
+    api.rotary(shape, plan, pos, k=k, out=(None, k))
+    assert torch.equal(k[:, :, -n:], want) and not k[:, :, :-n].any()
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+def test_tree_verify_rows_past_32_bits(drawn):
+    """1024 sequences of the largest vocabulary: the last ones' rows begin past 2^31 entries."""
+    B, T, V = 1024, 3, 1 << 20
+    rng = np.random.default_rng(2)
+    target = torch.zeros((B, T, V), device="cuda")
+    draft = torch.zeros((B, T, V), device="cuda") if drawn else None
+    at = rng.integers(0, V, size=(B, T, 4))
+    p, q = (np.tile(np.array(x, dtype=np.float32) / 16, (B, T, 1)) for x in ((8, 4, 3, 1), (2, 2, 6, 6)))
+    for b in range(B):
+        for t in range(T):
+            at[b, t] = np.sort(rng.choice(V, 4, replace=False))
+    rows = torch.as_tensor(at).cuda()
+    target.scatter_(2, rows, dev(p))
+    if drawn:
+        draft.scatter_(2, rows, dev(q))
+    tokens = np.zeros((B, T), dtype=np.int32)
+    tokens[:, 1], tokens[:, 2] = at[np.arange(B), 0, rng.integers(0, 4, B)], at[np.arange(B), 1, rng.integers(0, 4, B)]
+    u = np.minimum(rng.random((B, T)).astype(np.float32), np.float32(1 - 2.0 ** -24))
+    ws = api.Workspace(256)
+    got = [x.cpu().numpy() for x in api.tree_verify(dev(tokens, torch.int32), None, dev(u), target, draft, workspace=ws)]
+    assert ws.errors() == 0
+    del target, draft
+    # the same over the entries that have weight
+    for b in list(range(0, 1024, 41)) + [1021, 1022, 1023]:
+        # tokens as their places in the four of their parent's row
+        of = [0] + [int(np.where(at[b, t - 1] == tokens[b, t])[0][0]) for t in (1, 2)]
+        a, path, nxt = R.tree_verify(of, [-1, 0, 1], u[b].astype(np.float64), p[b].astype(np.float64), q[b].astype(np.float64) if drawn else None, T)
+        assert got[0][b] == a and list(got[1][b]) == path + [-1] * (T - a) and got[2][b] == at[b, path[-1], nxt]
